@@ -1,0 +1,204 @@
+"""Thin Python binding of the attention calls (``include/ecfa.h``): what lies between a layer's compressed projections.
+
+Argument marshalling only; every step runs inside ``libecf8.so`` (importing this module fails loudly when the library is
+not built).  The objects here hold the C structures and keep the tensors they point to alive: a ``Cache`` and a ``Batch`` are
+made once and used by every layer's and every step's calls; the tensors inside them may be rewritten in place.
+"""
+import ctypes
+
+import torch
+
+from . import ecf8 as _e
+
+_lib = _e._lib
+F32, BF16, E4M3 = 1, 2, 3
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_RAMP = 0, 1, 2, 3
+_vp, _u64, _u32, _i64, _f32 = ctypes.c_void_p, ctypes.c_uint64, ctypes.c_uint32, ctypes.c_int64, ctypes.c_float
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("d", _vp), ("token_stride", _i64), ("head_stride", _i64), ("heads", _u32), ("dtype", _u32)]
+
+
+class _Cache(ctypes.Structure):
+    _fields_ = [("d_k", _vp), ("d_v", _vp), ("d_k_scale", _vp), ("d_v_scale", _vp), ("k_stride", _i64 * 3), ("v_stride", _i64 * 3),
+                ("n_pages", _u32), ("page_size", _u32), ("kv_heads", _u32), ("head_dim", _u32), ("dtype", _u32), ("reserved", _u32)]
+
+
+class _Batch(ctypes.Structure):
+    _fields_ = [("d_page_table", _vp), ("d_kv_len", _vp), ("d_q_start", _vp), ("table_stride", _i64), ("table_width", _u32),
+                ("n_seqs", _u32), ("n_tokens", _u32), ("max_q", _u32), ("max_kv", _u32), ("reserved", _u32)]
+
+
+class _Rope(ctypes.Structure):
+    _fields_ = [("d_freq", _vp), ("d_pos", _vp), ("rot_dim", _u32), ("interleaved", _u32), ("scale", _f32), ("reserved", _u32)]
+
+
+class _AttendOpts(ctypes.Structure):
+    _fields_ = [("scale", _f32), ("softcap", _f32), ("d_slopes", _vp), ("d_prefix_len", _vp), ("causal", _u32), ("window", _u32)]
+
+
+_P = ctypes.POINTER
+_lib.ecfa_rope_freq.argtypes = [_u32, ctypes.c_double, _u32, ctypes.c_double, ctypes.c_double, ctypes.c_double, ctypes.c_double, _P(_u64), _P(_f32)]
+_lib.ecfa_append.argtypes = [_P(_Cache), _P(_Batch), _P(_Rope), _P(_Rows), _P(_Rows), _P(_Rows), _P(_Rows), _vp]
+_lib.ecfa_attend_workspace_bytes.argtypes = [_P(_Cache), _P(_Batch), _u32]
+_lib.ecfa_attend_workspace_bytes.restype = _u64
+_lib.ecfa_attend.argtypes = [_P(_Cache), _P(_Batch), _P(_AttendOpts), _P(_Rows), _P(_Rows), _vp, _u64, _vp]
+_lib.ecfa_quant.argtypes = [_vp, _u32, _u64, _u64, _i64, _u32, _vp, _vp, _vp]
+
+_DTYPE = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def _bad(fn):
+    return _e.Ecf8Error(fn, _e.E_ARG)
+
+
+def _rows(fn, x, n_tokens, heads, dim):
+    """A (tokens, heads, dim) tensor as the C structure: any strides, elements of a head next to each other."""
+    if x.dim() != 3 or x.shape[0] != n_tokens or x.shape[2] != dim or (heads and x.shape[1] != heads) or x.dtype not in _DTYPE:
+        raise _bad(fn)
+    s = x.stride()
+    if s[2] != 1:
+        raise _bad(fn)
+    return _Rows(x.data_ptr(), s[0], s[1], x.shape[1], _DTYPE[x.dtype])
+
+
+def _i32(fn, t, shape):
+    if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous():
+        raise _bad(fn)
+    return t.data_ptr()
+
+
+def _scale_ptr(t, heads):
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or tuple(t.shape) != (heads,) or not t.is_contiguous():
+        raise _bad("Cache")
+    return t.data_ptr()
+
+
+class Cache:
+    """A pool of pages: k and v are (pages, page_size, kv_heads, head_dim) tensors of BF16 or E4M3 (``torch.float8_e4m3fn``, or uint8
+    holding its bytes), of any strides over the first three dimensions; k_scale and v_scale (kv_heads,) fp32 or None."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.stride(3) != 1 or v.stride(3) != 1:
+            raise _bad("Cache")
+        if k.dtype == torch.bfloat16:
+            dtype = BF16
+        elif k.dtype in (torch.float8_e4m3fn, torch.uint8):
+            dtype = E4M3
+        else:
+            raise _bad("Cache")
+        pages, page, heads, dim = k.shape
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.c = _Cache(k.data_ptr(), v.data_ptr(), _scale_ptr(k_scale, heads), _scale_ptr(v_scale, heads), (_i64 * 3)(*k.stride()[:3]),
+                        (_i64 * 3)(*v.stride()[:3]), pages, page, heads, dim, dtype, 0)
+        self.kv_heads, self.head_dim, self.device = heads, dim, k.device
+
+
+class Batch:
+    """One step of a serving loop, over tensors that the loop rewrites in place: page_table (seqs, width) int32, kv_len (seqs,) int32
+    with the new tokens counted, q_start (seqs + 1,) int32 (None: one new token each).  n_tokens: rows of q, k, v and out (default with
+    q_start None: seqs).  max_q, max_kv: the most new tokens and keys of a sequence, hints for how the work is split."""
+
+    def __init__(self, page_table, kv_len, q_start=None, n_tokens=None, max_q=0, max_kv=0):
+        if page_table.dim() != 2 or page_table.dtype != torch.int32 or page_table.stride(1) != 1:
+            raise _bad("Batch")
+        seqs, width = page_table.shape
+        if n_tokens is None:
+            if q_start is not None:
+                raise _bad("Batch")
+            n_tokens = seqs
+        self.page_table, self.kv_len, self.q_start = page_table, kv_len, q_start
+        self.n_tokens = n_tokens
+        self.c = _Batch(page_table.data_ptr(), _i32("Batch", kv_len, (seqs,)), None if q_start is None else _i32("Batch", q_start, (seqs + 1,)),
+                        page_table.stride(0), width, seqs, n_tokens, max_q, max_kv, 0)
+
+
+def rope_freq(rot_dim, base=10000.0, kind=ROPE_PLAIN, factor=1.0, original_len=0.0, beta_fast=32.0, beta_slow=1.0, device="cuda"):
+    """(frequencies as int64 bit patterns on the device, scale) of ``ecfa_rope_freq``: what a ``Rope`` takes."""
+    freq, scale = (_u64 * max(1, rot_dim // 2))(), _f32()
+    _e._check("ecfa_rope_freq", _lib.ecfa_rope_freq(rot_dim, base, kind, factor, original_len, beta_fast, beta_slow, freq, ctypes.byref(scale)))
+    return torch.tensor([int(f) for f in freq], dtype=torch.int64).to(device), float(scale.value)
+
+
+class Rope:
+    """The rotation: freq (rot_dim / 2,) int64 as ``rope_freq`` gives it; pos (n_tokens,) int32 where positions are not the
+    places in the cache."""
+
+    def __init__(self, freq, interleaved=False, scale=1.0, pos=None):
+        if freq.dim() != 1 or freq.dtype != torch.int64 or not freq.is_contiguous():
+            raise _bad("Rope")
+        self.freq, self.pos = freq, pos
+        self.c = _Rope(freq.data_ptr(), None if pos is None else _i32("Rope", pos, tuple(pos.shape)), 2 * freq.numel(), int(interleaved), scale, 0)
+
+
+def ecfa_append(cache, batch, k=None, v=None, q=None, q_out=None, rope=None, stream=None):
+    """k turned and v into the cache, q turned into q_out (allocated if absent), which is returned.  k, v: (n_tokens, kv_heads,
+    head_dim), q: (n_tokens, heads, head_dim), all fp32 or all BF16."""
+    n, dim = batch.n_tokens, cache.head_dim
+    if rope is not None and rope.pos is not None and rope.pos.numel() != n:
+        raise _bad("ecfa_append")
+    rk = None if k is None else _rows("ecfa_append", k, n, cache.kv_heads, dim)
+    rv = None if v is None else _rows("ecfa_append", v, n, cache.kv_heads, dim)
+    rq = ro = None
+    if q is not None:
+        rq = _rows("ecfa_append", q, n, 0, dim)
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+        ro = _rows("ecfa_append", q_out, n, q.shape[1], dim)
+    elif q_out is not None:
+        raise _bad("ecfa_append")
+    rc = _lib.ecfa_append(cache.c, batch.c, None if rope is None else rope.c, rq, rk, rv, ro, _e._stream_ptr(stream))
+    _e._check("ecfa_append", rc)
+    return q_out
+
+
+def attend_workspace(cache, batch, heads):
+    """A workspace for ``ecfa_attend`` with `heads` query heads on this batch (a uint8 tensor, for one call at a time), or None if the calls
+    need none."""
+    n = int(_lib.ecfa_attend_workspace_bytes(cache.c, batch.c, heads))
+    return torch.empty(n, dtype=torch.uint8, device=cache.device) if n else None
+
+
+def ecfa_attend(cache, batch, q, scale=None, causal=True, window=0, softcap=0.0, slopes=None, prefix=None, out=None, workspace=None, stream=None):
+    """Attention of the batch's new tokens over the cache; q and the result (n_tokens, heads, head_dim) BF16.  scale defaults to
+    head_dim^-0.5; slopes (heads,) fp32; prefix (seqs,) int32.  Without a workspace one is allocated for the call where it needs it."""
+    n, dim = batch.n_tokens, cache.head_dim
+    rq = _rows("ecfa_attend", q, n, 0, dim)
+    heads = q.shape[1]
+    if out is None:
+        out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+    ro = _rows("ecfa_attend", out, n, heads, dim)
+    if slopes is not None and (slopes.dtype != torch.float32 or tuple(slopes.shape) != (heads,) or not slopes.is_contiguous()):
+        raise _bad("ecfa_attend")
+    if workspace is None:
+        workspace = attend_workspace(cache, batch, heads)
+        if workspace is not None and stream is not None:
+            workspace.record_stream(stream)
+    opts = _AttendOpts(dim ** -0.5 if scale is None else scale, softcap, None if slopes is None else slopes.data_ptr(),
+                       None if prefix is None else _i32("ecfa_attend", prefix, tuple(batch.kv_len.shape)), int(causal), window)
+    rc = _lib.ecfa_attend(cache.c, batch.c, opts, rq, ro, None if workspace is None else workspace.data_ptr(),
+                          0 if workspace is None else workspace.numel(), _e._stream_ptr(stream))
+    _e._check("ecfa_attend", rc)
+    return out
+
+
+def ecfa_quant(x, group=0, q=None, scale=None, stream=None):
+    """x (rows, cols) fp32 or BF16, rows of any stride, to (E4M3 (rows, cols), fp32 scales (rows,) or with group = 128 (rows, cols / 128));
+    the result is a ``torch.float8_e4m3fn`` tensor unless q is given (uint8 or float8_e4m3fn, dense)."""
+    if x.dim() != 2 or x.dtype not in _DTYPE or (x.shape[1] > 1 and x.stride(1) != 1) or group not in (0, 128):
+        raise _bad("ecfa_quant")
+    rows, cols = x.shape
+    want = (rows, cols // 128) if group else (rows,)
+    if q is None:
+        q = torch.empty((rows, cols), dtype=torch.float8_e4m3fn, device=x.device)
+    if scale is None:
+        scale = torch.empty(want, dtype=torch.float32, device=x.device)
+    if (q.dtype not in (torch.float8_e4m3fn, torch.uint8) or tuple(q.shape) != (rows, cols) or not q.is_contiguous()
+            or scale.dtype != torch.float32 or tuple(scale.shape) != want or not scale.is_contiguous()):
+        raise _bad("ecfa_quant")
+    _e._check("ecfa_quant", _lib.ecfa_quant(x.data_ptr(), _DTYPE[x.dtype], rows, cols, x.stride(0), group, q.data_ptr(), scale.data_ptr(),
+                                            _e._stream_ptr(stream)))
+    return q, scale

@@ -1,0 +1,370 @@
+"""ecfa_attend against the definition in 64 bits: lengths from nothing to past a step and past a split, heads shared and not, head sizes
+that fill no register, pages that end inside a step, both cache types and both orders, masks that leave rows without a key, what is
+stored in places that nobody sees, hints that are wrong, other streams, graphs, and pools that 32 bits cannot address."""
+import itertools
+
+import numpy as np
+import pytest
+import torch
+
+import attention_reference as ref
+from paper_2510_02676_amd import ecf8, ecfa
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+class Setting:
+    """A pool, a table in no order and a batch; `kv` and `qn` a length each per sequence."""
+
+    def __init__(self, kv, qn, heads=8, kv_heads=2, dim=128, page=16, cache="bf16", order="token", seed=0, holes=(), width=None, single=False, scales=True,
+                 hints=True):
+        g = torch.Generator().manual_seed(seed)
+        self.page, self.kv, self.qn, self.heads = page, kv, qn, heads
+        need = [-(-max(0, n) // page) for n in kv]
+        width = max(max(need), 1) if width is None else width
+        pages = sum(need) + 2
+        ids = torch.randperm(pages, generator=g).tolist()
+        self.table = [[-1] * width for _ in kv]
+        for s, n in enumerate(need):
+            for j in range(min(n, width)):
+                self.table[s][j] = ids.pop()
+        for s, j, what in holes:
+            self.table[s][j] = what
+        self.q_start = [0] + list(itertools.accumulate(qn))
+        k, v = (torch.randn((pages, page, kv_heads, dim), generator=g) for _ in range(2))
+        self.k_scale = self.v_scale = None
+        if cache == "e4m3":
+            if scales:
+                self.k_scale, self.v_scale = (torch.rand(kv_heads, generator=g) * 0.02 + 0.005 for _ in range(2))
+                k, v = k / self.k_scale[:, None], v / self.v_scale[:, None]
+            k, v = (x.clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8) for x in (k, v))
+        else:
+            k, v = k.bfloat16(), v.bfloat16()
+        if order == "head":
+            k, v = (x.transpose(1, 2).contiguous().transpose(1, 2) for x in (k, v))
+        self.k, self.v, self.pages = k, v, pages
+        self.q = (torch.randn((self.q_start[-1], heads, dim), generator=g) * 2).bfloat16()
+        self.single, self.hints = single, hints
+
+    def batch(self, **more):
+        i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+        hints = dict(max_q=max(self.qn), max_kv=max(max(self.kv), 1)) if self.hints else {}
+        return ecfa.Batch(i32(self.table), i32(self.kv), None if self.single else i32(self.q_start), n_tokens=self.q_start[-1], **{**hints, **more})
+
+    def device_cache(self):
+        up = lambda x: None if x is None else x.to(DEV)  # noqa: E731
+        k, v = (torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=DEV).copy_(x) for x in (self.k, self.v))
+        return ecfa.Cache(k, v, up(self.k_scale), up(self.v_scale))
+
+    def run(self, **opts):
+        q = self.q.to(DEV)
+        out = torch.full((q.shape[0] + 2, *q.shape[1:]), float("nan"), dtype=torch.bfloat16, device=DEV)
+        ecfa.ecfa_attend(self.device_cache(), self.batch(), q, out=out[1:-1], **opts)
+        torch.cuda.synchronize()
+        assert torch.isnan(out[0]).all() and torch.isnan(out[-1]).all()
+        return out[1:-1].cpu().double().numpy()
+
+    def want(self, scale=None, causal=True, window=0, softcap=0.0, slopes=None, prefix=None):
+        toks = ref.tokens(self.q_start, self.kv, self.table, self.page, self.pages)
+        return ref.attend(self.q, ref.values(self.k, self.k_scale), ref.values(self.v, self.v_scale), toks, self.q.shape[2] ** -0.5 if scale is None else scale,
+                          causal, window, softcap, None if slopes is None else slopes.cpu().numpy(), None if prefix is None else prefix.tolist())
+
+
+def check(setting, **opts):
+    got = setting.run(**opts)
+    want, size = setting.want(**opts)
+    bad = ~(np.abs(got - want) <= ref.attend_bound(want, size))
+    assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:4].tolist(), float(np.abs(got - want).max()))
+    return got, want
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("dim", [16, 48, 64, 80, 96, 112, 128, 160, 192, 256])
+def test_head_sizes(dim, cache):
+    check(Setting([37, 5], [3, 2], dim=dim, cache=cache, seed=dim))
+    check(Setting([70, 5], [30, 5], heads=4, kv_heads=1, dim=dim, cache=cache, seed=dim))
+
+
+@pytest.mark.parametrize("kv", [0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 257, 700, 1500])
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+def test_single_tokens(kv, cache):
+    check(Setting([kv, max(0, kv - 1), 3], [1, 1, 1], cache=cache, single=True, seed=kv))
+
+
+@pytest.mark.parametrize("n", [1, 2, 3, 4, 5, 8, 9, 15, 16, 17, 31, 32, 33, 40, 63, 65, 129, 200])
+@pytest.mark.parametrize("more", [0, 1, 77])
+def test_chunks(n, more):
+    check(Setting([n + more, 40, 0], [n, 1, 0], cache="e4m3" if n % 2 else "bf16", seed=n))
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (3, 1), (5, 5), (15, 5), (16, 1), (17, 1), (32, 2), (33, 1), (71, 1), (12, 12), (128, 1)])
+@pytest.mark.parametrize("qn", [1, 6, 45])
+def test_heads_shared_and_not(heads, kv_heads, qn):
+    check(Setting([60, 9], [qn, 2], heads=heads, kv_heads=kv_heads, dim=64, seed=heads))
+
+
+@pytest.mark.parametrize("page", [1, 2, 4, 8, 16, 32, 128, 256])
+@pytest.mark.parametrize("order", ["token", "head"])
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+def test_pages(page, order, cache):
+    check(Setting([1, 150, 33], [1, 21, 2], page=page, order=order, cache=cache, heads=4, seed=page))
+    check(Setting([1, 150, 300], [1, 1, 1], page=page, order=order, cache=cache, single=True, seed=page))
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("qn,kv", [([1, 1, 1], [90, 1, 200]), ([40, 1, 13], [90, 7, 200]), ([130, 3, 66], [140, 3, 300])])
+def test_masks_and_scores(qn, kv, cache):
+    make = lambda: Setting(kv, qn, cache=cache, seed=sum(kv))  # noqa: E731
+    slopes = 2.0 ** -torch.arange(1, 9, dtype=torch.float32, device=DEV)
+    prefix = torch.tensor([60, 0, 1000], dtype=torch.int32, device=DEV)
+    check(make(), causal=False)
+    for window in (1, 7, 32, 33, 64, 1000, 2 ** 32 - 1):
+        check(make(), window=window)
+        check(make(), window=window, causal=False)
+    check(make(), softcap=2.0)
+    check(make(), softcap=50.0, scale=0.3)
+    check(make(), slopes=slopes)
+    check(make(), slopes=slopes, causal=False, softcap=5.0)
+    check(make(), prefix=prefix)
+    check(make(), prefix=prefix, slopes=slopes, softcap=5.0)
+
+
+def test_rows_without_a_key_are_zeros():
+    # more new tokens than the cache holds: the first ones come before every key; and sequences of nothing
+    s = Setting([5, 0, 2, -3], [9, 3, 1, 2])
+    got, want = check(s)
+    assert not got[:4].any() and not got[9:12].any() and not got[13:].any() and got[4:9].any()
+    # all pages of a sequence are holes
+    s = Setting([40, 40], [2, 2], holes=[(0, j, -1) for j in range(3)])
+    got, _ = check(s)
+    assert not got[:2].any() and got[2:].any()
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+def test_holes_and_pages_that_are_none(cache):
+    s = Setting([200, 100], [30, 1], cache=cache, holes=[(0, 1, -1), (0, 4, 10 ** 6), (0, 12, -2 ** 31), (1, 0, 2 ** 31 - 1)])
+    check(s)
+    check(s, causal=False)
+    # a table that is narrower than the sequence: what it does not name is not seen
+    check(Setting([200, 100], [30, 1], cache=cache, width=5))
+
+
+def poison(s, where, what):
+    """Puts `what` into V and K of one key of a sequence."""
+    seq, key = where
+    p, at = s.table[seq][key // s.page], key % s.page
+    for x in (s.k, s.v):
+        if x.dtype == torch.uint8:
+            x[p, at] = 0x7F
+        else:
+            x[p, at] = what
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("qn", [1, 3, 20, 70])
+@pytest.mark.parametrize("what", [float("nan"), float("inf"), -float("inf")])
+def test_what_is_not_seen_does_not_matter(cache, qn, what):
+    """NaN and infinities behind the end of a sequence, before a window, and in keys that only later tokens see; tokens that do see them
+    get what the definition says."""
+    s = Setting([85, 85], [qn, qn], cache=cache, seed=5)
+    clean = s.run()
+    for page in range(s.pages):                                 # everything that belongs to nobody
+        for at in range(s.page):
+            if not any(t[j // s.page] == page and j % s.page == at for t in s.table for j in range(85)):
+                s.k[page, at] = 0x7F if cache == "e4m3" else what
+                s.v[page, at] = 0xFF if cache == "e4m3" else what
+    assert np.array_equal(s.run(), clean)
+    check(s)
+    # the newest key of sequence 0: only its last token sees it; the others' sums may be made in another order
+    want, size = s.want()
+    poison(s, (0, 84), what)
+    got = s.run()
+    assert np.array_equal(got[qn:], clean[qn:]) and np.isnan(got[qn - 1]).all()
+    assert (np.abs(got - want) <= ref.attend_bound(want, size))[:qn - 1].all()
+    # an old key of sequence 1, outside of everybody's window
+    s = Setting([85, 85], [qn, qn], cache=cache, seed=5)
+    clean = s.run(window=10)
+    poison(s, (1, 85 - qn - 10), what)
+    assert np.array_equal(s.run(window=10), clean)
+    # in a value alone, where the weights are finite: an infinity reaches the tokens that see it, in its element
+    if cache == "bf16":
+        s = Setting([85, 85], [qn, qn], cache=cache, seed=5)
+        key = 85 - (qn + 1) // 2
+        s.v[s.table[0][key // s.page], key % s.page, 1, 9] = what
+        want, size = s.want()
+        got = s.run()
+        hit = np.zeros(got.shape, dtype=bool)
+        hit[qn - (85 - key):qn, 4:, 9] = True
+        assert (np.abs(got - want) <= ref.attend_bound(want, size))[~hit].all()
+        assert (np.isnan(got[hit]) if what != what else got[hit] == what).all()
+
+
+def test_large_scores():
+    """Weights of one key against all others, and scores far below the rest, in and out of the first step."""
+    s = Setting([300, 40], [5, 1], heads=2, kv_heads=1, dim=64)
+    s.q *= 40
+    check(s)
+    check(s, scale=1e-6)
+
+
+def test_hints_do_not_change_what_is_computed():
+    s = Setting([300, 40, 900], [45, 1, 2])
+    want, size = s.want()
+    cache, q = s.device_cache(), s.q.to(DEV)
+    for max_q, max_kv in ((0, 0), (1, 1), (2, 64), (45, 900), (10 ** 6, 10 ** 6), (3, 10 ** 9)):
+        b = s.batch(max_q=max_q, max_kv=max_kv)
+        got = ecfa.ecfa_attend(cache, b, q)
+        again = ecfa.ecfa_attend(cache, b, q)
+        torch.cuda.synchronize()
+        assert torch.equal(got, again)
+        assert (np.abs(got.cpu().double().numpy() - want) <= ref.attend_bound(want, size)).all(), (max_q, max_kv)
+
+
+def test_starts_that_are_wrong_stay_inside():
+    """Starts beyond the rows, falling or negative ones: rows that belong to a sequence by them are written, no others."""
+    s = Setting([60, 60], [4, 4])
+    q, out = s.q.to(DEV), torch.full((10, 8, 128), 7.0, dtype=torch.bfloat16, device=DEV)
+    for starts in ([0, 4, 1000], [-5, 4, 8], [6, 2, 8], [0, 2 ** 31 - 1, -2 ** 31], [8, 8, 8]):
+        b = s.batch()
+        b.q_start.copy_(torch.tensor(starts, dtype=torch.int32))
+        ecfa.ecfa_attend(s.device_cache(), b, q, out=out[1:9])
+        torch.cuda.synchronize()
+        assert (out[0] == 7).all() and (out[9] == 7).all() and not torch.isnan(out).any()
+
+
+def test_strides():
+    """q and out as parts of wider rows, heads apart, and pools that are parts of larger ones."""
+    s = Setting([75, 33], [9, 1], heads=4, kv_heads=2, dim=96)
+    want, size = s.want()
+    wide = torch.full((10, 3, 4, 112), float("nan"), dtype=torch.bfloat16, device=DEV)
+    wide[:, 1, :, 8:104] = s.q.to(DEV)
+    q = wide[:, 1, :, 8:104]
+    out = torch.zeros((4, 10, 104), dtype=torch.bfloat16, device=DEV).transpose(0, 1)[:, :, 8:]
+    pool = torch.full((2, s.pages, 3, 16, 2, 128), float("nan"), dtype=torch.bfloat16, device=DEV)
+    k, v = pool[0, :, 2, :, :, 16:112], pool[1, :, 0, :, :, 32:]
+    k.copy_(s.k)
+    v.copy_(s.v)
+    ecfa.ecfa_attend(ecfa.Cache(k, v), s.batch(), q, out=out)
+    torch.cuda.synchronize()
+    assert (np.abs(out.cpu().double().numpy() - want) <= ref.attend_bound(want, size)).all()
+
+
+def test_many_sequences():
+    kv = [(i * 37) % 90 for i in range(150)]
+    check(Setting(kv, [1] * 150, heads=2, kv_heads=1, dim=64, single=True))
+    qn = [(i * 7) % 5 for i in range(150)]
+    check(Setting([max(a, b) for a, b in zip(kv, qn)], qn, heads=2, kv_heads=1, dim=64))
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+def test_long_sequences(cache):
+    """Past many splits; against 32-bit torch on the device in one piece, whose own error is far below the bound."""
+    s = Setting([20011, 3], [1, 1], heads=8, kv_heads=2, cache=cache, single=True, page=64)
+    s2 = Setting([6007, 3], [200, 1], heads=8, kv_heads=2, cache=cache, page=64)
+    for x in (s, s2):
+        got = x.run()
+        k, v = (torch.from_numpy(ref.values(p, sc)).to(DEV) for p, sc in ((x.k, x.k_scale), (x.v, x.v_scale)))
+        key = torch.arange(x.kv[0])
+        slot = torch.tensor(x.table[0])[key // 64]
+        k, v = k[slot, key % 64], v[slot, key % 64]              # (keys, kv_heads, dim), 64 bits
+        for h in range(8):
+            sc = x.q[:x.qn[0], h].to(DEV).double() @ k[:, h // 4].T * 128 ** -0.5
+            place = torch.arange(x.kv[0] - x.qn[0], x.kv[0], device=DEV)
+            sc.masked_fill_(key.to(DEV)[None, :] > place[:, None], -float("inf"))
+            w = torch.softmax(sc, -1)
+            want, size = (w @ v[:, h // 4]).cpu().numpy(), (w @ v[:, h // 4].abs()).cpu().numpy()
+            assert (np.abs(got[:x.qn[0], h] - want) <= ref.attend_bound(want, size)).all()
+
+
+def test_a_pool_beyond_32_bits():
+    """Pages more than 2^32 bytes into the pool."""
+    pages, page, heads, dim = 1 << 17, 32, 8, 128                # 8 GiB of keys and as much of values
+    k = torch.empty((pages, page, heads, dim), dtype=torch.bfloat16, device=DEV)
+    v = torch.empty_like(k)
+    s = Setting([90, 50], [1, 20], heads=16, kv_heads=8, dim=dim, page=page)
+    far = {p: pages - 1 - 5000 * i for i, p in enumerate(sorted({p for t in s.table for p in t if p >= 0}))}
+    for p, f in far.items():
+        k[f].copy_(s.k[p])
+        v[f].copy_(s.v[p])
+    want, size = s.want()
+    s.table = [[far.get(p, -1) for p in t] for t in s.table]
+    got = ecfa.ecfa_attend(ecfa.Cache(k, v), s.batch(), s.q.to(DEV)).cpu().double().numpy()
+    assert (np.abs(got - want) <= ref.attend_bound(want, size)).all()
+    # and the same places written by append
+    new = torch.randn((21, 8, dim), device=DEV)
+    ecfa.ecfa_append(ecfa.Cache(k, v), s.batch(), new, -new)
+    for t, (seq, place, slots) in enumerate(ref.tokens(s.q_start, s.kv, s.table, page, pages)):
+        p, at = slots[place]
+        assert torch.equal(k[p, at], new[t].bfloat16()) and torch.equal(v[p, at], -new[t].bfloat16())
+
+
+def test_another_stream_and_a_shared_pool():
+    s = Setting([400, 90], [1, 1], single=True)
+    cache, b, q = s.device_cache(), s.batch(), s.q.to(DEV)
+    want = ecfa.ecfa_attend(cache, b, q)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(20):
+        with torch.cuda.stream(side):
+            got = ecfa.ecfa_attend(cache, b, q)
+        other = ecfa.ecfa_attend(cache, b, q, stream=side)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and torch.equal(other, want)
+
+
+def test_a_captured_step_follows_its_tensors():
+    """Append, attend and quant in one graph; lengths, tables and inputs are rewritten between replays."""
+    s = Setting([10, 300], [1, 1], single=True, width=40)
+    used = {p for t in s.table for p in t}
+    free = [p for p in range(s.pages) if p not in used]
+    s.table[0][1] = free[0]                                      # room for the steps to come
+    if s.table[1][19] < 0:
+        s.table[1][19] = free[1]
+    cache, b = s.device_cache(), s.batch()
+    g = torch.Generator().manual_seed(3)
+    q, k, v = (torch.randn((2, h, 128), generator=g).to(DEV) for h in (8, 2, 2))
+    rope = ecfa.Rope(ecfa.rope_freq(128)[0].to(DEV))
+    work = ecfa.attend_workspace(cache, b, 8)
+    turned, out = (torch.empty((2, 8, 128), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    e4, sc = torch.empty((2, 1024), dtype=torch.uint8, device=DEV), torch.empty((2,), device=DEV)
+
+    def step(cache):
+        ecfa.ecfa_append(cache, b, k, v, q, turned, rope)
+        ecfa.ecfa_attend(cache, b, turned, out=out, workspace=work)
+        ecfa.ecfa_quant(out.view(2, 1024), q=e4, scale=sc)
+
+    step(cache)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(cache)
+    for i in range(4):
+        for x in (q, k, v):
+            x.copy_(torch.randn(x.shape, generator=g))
+        b.kv_len.copy_(torch.tensor([10 + i, 300 + i], dtype=torch.int32))
+        twin = ecfa.Cache(cache.k.clone(), cache.v.clone())
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [x.clone() for x in (turned, out, e4, sc, cache.k, cache.v)]
+        for x in (turned, out, e4, sc):
+            x.zero_()
+        step(twin)
+        torch.cuda.synchronize()
+        for a, c in zip(got, (turned, out, e4, sc, twin.k, twin.v)):
+            assert torch.equal(a, c)
+
+
+def test_a_workspace_that_is_too_small_or_missing():
+    s = Setting([5000], [1], single=True)
+    cache, b, q = s.device_cache(), s.batch(), s.q.to(DEV)
+    out = torch.full_like(q, 5.0)
+    work = ecfa.attend_workspace(cache, b, 8)
+    with pytest.raises(ecf8.Ecf8Error) as e:
+        ecfa.ecfa_attend(cache, b, q, out=out, workspace=work[:-4])
+    assert e.value.code == ecf8.E_CAPACITY
+    with pytest.raises(ecf8.Ecf8Error) as e:
+        ecfa.ecfa_attend(cache, b, q, out=out, workspace=torch.empty(work.numel() + 16, dtype=torch.uint8, device=DEV)[8:])
+    assert e.value.code == ecf8.E_ALIGN
+    torch.cuda.synchronize()
+    assert (out == 5).all()
