@@ -23,13 +23,26 @@ struct AttendArgs {
     int64_t q_tok, q_head, o_tok, o_head;    // bytes
     const float *slopes;
     const int32_t *prefix;
-    float *part;                             // partial sums: [row of (token, head)][split][head_dim], then (m, l) pairs
-    float *part_ml;
+    float *part;                             // partial sums of a row's splits, head_dim each: see few_part, many_part
+    float *part_ml;                          // (m, l) of each
+    int64_t many_part0;                      // where those of the tiles of many rows begin
     float scale_log2;                        // scale * log2(e)
     float cap;                               // softcap, 0: none
     uint32_t head_dim, heads, kv_heads, share, causal, window;
-    uint32_t splits, row_tiles, tile_rows, split_unit;   // of a launch
+    int32_t few_rows;                        // sequences of up to so many rows are the few-rows kernel's, the others the many-rows kernel's
+    uint32_t few_tile, few_splits;           // rows of a tile; splits of the first tile of a sequence (others, where there are any, have one)
+    uint32_t many_tiles, many_splits;
 };
+
+// The partial sums of a row's first split.
+__device__ inline int64_t few_part(const AttendArgs &a, uint32_t s, uint32_t kvh, int32_t row)
+{
+    return (((int64_t)s * a.kv_heads + kvh) * a.few_tile + row) * a.few_splits;
+}
+__device__ inline int64_t many_part(const AttendArgs &a, int64_t t, uint32_t head) { return a.many_part0 + (t * a.heads + head) * a.many_splits; }
+
+constexpr int FEW_WAVES = 4, FEW_UNIT = FEW_WAVES;               // steps of 32 keys that a split is a multiple of
+constexpr int MANY_WAVES = 4, MANY_ROWS = 32 * MANY_WAVES, MANY_KEYS = 64, MANY_UNIT = MANY_KEYS / 32;
 
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float NONE = -__builtin_huge_valf();
@@ -127,6 +140,13 @@ __device__ inline float capped(float x_log2, float cap)
     return (__builtin_fabsf(y) < 0.06f ? small : t) * (cap * LOG2E);
 }
 
+// Two numbers to BF16, nearest even, in one instruction.
+__device__ inline bf16x2 bf16_pair(float x, float y)
+{
+    typedef __attribute__((ext_vector_type(2))) float f32x2;
+    return __builtin_convertvector((f32x2{x, y}), bf16x2);
+}
+
 // Eight E4M3 bytes as BF16, which holds each of them.
 __device__ inline bf16x8 bf16_of_e4m3(uint32_t lo, uint32_t hi)
 {
@@ -143,8 +163,68 @@ __device__ inline void lds_fence_wave()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+// The slow way for one row: key by key, in fp32, from memory.  Taken where a value that some rows of a tile see and others do not
+// is NaN or infinite: the matrix cores would multiply it by the zero weight of the rows that do not see it.  PARTS lanes
+// (lane / (64 / PARTS) of them) share a row; element 8 (PARTS c + part) + .. of q and k is a lane's in dot products, and `element(n)`
+// names the n-th group of four elements of the result that it holds, in y[4 n ..].  Steps [step_a, step_b) of 32 keys.
+template <bool F8, int PARTS, int GROUPS, class Element>
+__device__ inline void attend_slowly(const AttendArgs &a, const uint8_t *q, const uint8_t *k0, const uint8_t *v0, const int32_t *table, int32_t step_a,
+                                     int32_t step_b, KeyRange seen, int32_t place, float to_log2, float slope, int part, Element element, float *y, float &m, float &l)
+{
+    const uint32_t in_page = (1u << a.c.page_shift) - 1;
+    const auto eight = [](const uint8_t *p, float *x) {        // of the cache, from the place of the first
+        bf16x8 b;
+        if constexpr (F8) b = bf16_of_e4m3(((const uint32_t *)p)[0], ((const uint32_t *)p)[1]);
+        else b = *(const bf16x8 *)p;
+        for (int i = 0; i < 8; i++) x[i] = (float)b[i];
+    };
+    constexpr int E = F8 ? 1 : 2;
+    m = NONE;
+    l = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4 * GROUPS; i++) y[i] = 0.f;
+#pragma unroll 1
+    for (int32_t key = 32 * step_a; key < 32 * step_b; key++) {
+        const bool in = key >= seen.lo && key < seen.hi;
+        const uint32_t page = in ? (uint32_t)table[(uint32_t)key >> a.c.page_shift] : 0xffffffffu;
+        const bool use = page < a.c.n_pages;
+        if (!__any(use)) continue;
+        const int64_t pg = use ? page : 0u, at = (uint32_t)key & in_page;
+        const uint8_t *k = k0 + pg * a.c.k_page + at * a.c.k_tok, *v = v0 + pg * a.c.v_page + at * a.c.v_tok;
+        float x = 0.f;
+#pragma unroll 1
+        for (int e = 8 * part; e < (int)a.head_dim; e += 8 * PARTS) {
+            float kk[8];
+            eight(k + e * E, kk);
+            const bf16x8 qq = *(const bf16x8 *)(q + 2 * e);
+            for (int i = 0; i < 8; i++) x += kk[i] * (float)qq[i];
+        }
+        for (int n = 64 / PARTS; n < 64; n *= 2) x += __shfl_xor(x, n);
+        x *= to_log2;
+        if (a.cap > 0.f) x = capped(x, a.cap);
+        const int32_t far = place - key;
+        x -= slope * (float)(far < 0 ? -far : far);
+        const float m_new = use ? max_f(m, x) : m, base = m_new == NONE ? 0.f : m_new;
+        const float shrink = exp2_fast(m - base), w = use ? (float)(__bf16)exp2_fast(x - base) : 0.f;
+        m = m_new;
+        l = l * shrink + w;
+#pragma unroll
+        for (int n = 0; n < GROUPS; n++) {
+            const int e = element(n);
+            float vv[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+            if (e < (int)a.head_dim) eight(v + (e & ~7) * E, vv);
+            for (int i = 0; i < 4; i++) {
+                const float z = y[4 * n + i] * shrink;
+                y[4 * n + i] = use ? z + w * (e & 4 ? vv[4 + i] : vv[i]) : z;
+            }
+        }
+    }
+}
+
 // Launches, one per cache type; kc = 32-element pieces of a head that the kernels are compiled for.
 int launch_few_rows_bf16(const AttendArgs &a, uint32_t kc, uint32_t tiles, hipStream_t s);
 int launch_few_rows_e4m3(const AttendArgs &a, uint32_t kc, uint32_t tiles, hipStream_t s);
+int launch_many_rows_bf16(const AttendArgs &a, uint32_t kc, hipStream_t s);
+int launch_many_rows_e4m3(const AttendArgs &a, uint32_t kc, hipStream_t s);
 
 } // namespace ecfa

@@ -12,21 +12,39 @@ constexpr int JOIN_THREADS = 256;
 
 // One workgroup for a (token, query head): the splits' (m, l, O) to one row.  The splits are dealt to groups of head_dim / 4 threads, so
 // that all partial rows are on their way at once.  Reads what the splits have written, 4 head_dim + 8 bytes each, once.
-__global__ __launch_bounds__(JOIN_THREADS) void ecfa_attend_join_kernel(const AttendArgs a)
+// The first few_blocks workgroups are for the rows of the few-rows kernel's first tiles, the others for tokens of the other kernel.
+__global__ __launch_bounds__(JOIN_THREADS) void ecfa_attend_join_kernel(const AttendArgs a, uint32_t few_blocks)
 {
     __shared__ f32x4 sums[JOIN_THREADS];
-    const uint32_t t = blockIdx.x / a.heads, head = blockIdx.x % a.heads;
-    const uint32_t s = seq_of_row(a.b, t);
+    __shared__ float alls[JOIN_THREADS];
+    const bool few = blockIdx.x < few_blocks;
+    uint32_t at = few ? blockIdx.x : blockIdx.x - few_blocks, s, head;
+    int32_t row, tile;                                         // of the sequence and its key/value head
+    if (few) {
+        row = (int32_t)(at % a.few_tile);
+        at /= a.few_tile;
+        s = at / a.kv_heads;
+        head = at % a.kv_heads * a.share + (uint32_t)row % a.share;
+        tile = (int32_t)a.few_tile;
+    } else {
+        head = at % a.heads;
+        s = seq_of_row(a.b, at / a.heads);
+        tile = MANY_ROWS;
+    }
     const Seq sq = seq_of(a.b, s);
-    const int32_t tok = (int32_t)t - sq.q0;
-    if (tok < 0 || tok >= sq.qn) return;
-    const int32_t rows = sq.qn * (int32_t)a.share, tile = (int32_t)a.tile_rows;
-    const int32_t row0 = (tok * (int32_t)a.share + (int32_t)(head % a.share)) / tile * tile;
-    const int32_t row_end = row0 + tile < rows ? row0 + tile : rows;
-    const KeyRange kr = keys_of(a, sq, prefix_of(a, s, sq), row0 / (int32_t)a.share, (row_end - 1) / (int32_t)a.share);
-    const int32_t used = split_of(kr, a.splits, (int32_t)a.split_unit).used;
+    const int32_t share = (int32_t)a.share, rows = sq.qn * share;
+    if (!few) {
+        const int32_t tok = (int32_t)(at / a.heads) - sq.q0;
+        if (tok < 0 || tok >= sq.qn) return;
+        row = tok * share + (int32_t)(head % a.share);
+    }
+    if (row >= rows || (rows <= a.few_rows) != few) return;
+    const int32_t row0 = row / tile * tile, row_end = row0 + tile < rows ? row0 + tile : rows;
+    const KeyRange kr = keys_of(a, sq, prefix_of(a, s, sq), row0 / share, (row_end - 1) / share);
+    const int32_t used = few ? split_of(kr, a.few_splits, FEW_UNIT).used : split_of(kr, a.many_splits, MANY_UNIT).used;
     if (used <= 1) return;                                     // the row is written already
-    const int64_t part = ((int64_t)t * a.heads + head) * a.splits;
+    const int64_t t = (int64_t)sq.q0 + row / share;
+    const int64_t part = few ? few_part(a, s, head / a.share, row) : many_part(a, t, head);
     const float *ml = a.part_ml + part * 2;
     float top = NONE;
     for (int32_t i = threadIdx.x & 63; i < used; i += 64) top = max_f(top, ml[2 * i]);
@@ -41,7 +59,6 @@ __global__ __launch_bounds__(JOIN_THREADS) void ecfa_attend_join_kernel(const At
             all += ml[2 * i + 1] * w;
             y += *(const f32x4 *)(a.part + (part + i) * a.head_dim + 4 * quad) * w;
         }
-    __shared__ float alls[JOIN_THREADS];
     sums[threadIdx.x] = y;
     alls[threadIdx.x] = all;
     __syncthreads();
@@ -53,46 +70,69 @@ __global__ __launch_bounds__(JOIN_THREADS) void ecfa_attend_join_kernel(const At
     const float inv = all == 0.f ? 0.f : 1.f / all;
     bf16x4 z;
     for (int i = 0; i < 4; i++) z[i] = (__bf16)(all == 0.f ? 0.f : y[i] * inv);
-    *(bf16x4 *)(a.out + (int64_t)t * a.o_tok + (int64_t)head * a.o_head + 8 * quad) = z;
+    *(bf16x4 *)(a.out + t * a.o_tok + (int64_t)head * a.o_head + 8 * quad) = z;
 }
 
 // What a call launches: decided by shapes and the hints alone.
 struct Shape {
-    uint32_t kc;                   // 32-element pieces of a head in the kernel
-    uint32_t tiles;                // sub-tiles of 16 rows
-    uint32_t row_tiles, splits, tile_rows, split_unit;
-    uint64_t part_floats;          // partial sums in the workspace, then two floats for each of part_rows
-    uint64_t part_rows;
+    uint32_t kc;                   // 32-element pieces of a head in the kernels
+    bool few, many;                // which kernels
+    int32_t few_rows;
+    uint32_t few_tiles, few_splits, many_tiles, many_splits;
+    uint64_t few_parts, many_parts;          // partial rows in the workspace
 };
 
 Shape shape_of(const ecfa_cache *c, const ecfa_batch *b, uint32_t heads, uint32_t cus)
 {
     Shape p{};
-    const uint32_t kc = (c->head_dim + 31) / 32;
+    const uint32_t kc = (c->head_dim + 31) / 32, share = heads / c->kv_heads;
     p.kc = kc <= 2 ? 2 : kc <= 4 ? kc : kc <= 6 ? 6 : 8;
     const uint32_t max_q = !b->d_q_start ? 1 : b->max_q && b->max_q < b->n_tokens ? b->max_q : b->n_tokens;
     const uint64_t keys = (uint64_t)b->table_width * c->page_size;
     const uint64_t max_kv = b->max_kv && b->max_kv < keys ? b->max_kv : keys;
-    const uint64_t rows = (uint64_t)max_q * (heads / c->kv_heads);
-    p.tiles = rows <= 16 ? 1 : 2;
-    p.tile_rows = 16 * p.tiles;
-    p.row_tiles = (uint32_t)((rows + p.tile_rows - 1) / p.tile_rows);
-    p.split_unit = 4;
-    // enough workgroups for four on each compute unit, of 128 keys at least
-    const uint64_t whole = (uint64_t)b->n_seqs * c->kv_heads * p.row_tiles;
-    const uint64_t want = whole ? (4ull * cus + whole - 1) / whole : 1, most = (max_kv + 127) / 128;
-    const uint64_t n = want < most ? want : most;
-    p.splits = (uint32_t)(n < 1 ? 1 : n > 256 ? 256 : n);
-    if (p.splits > 1) {
-        p.part_rows = (uint64_t)b->n_tokens * heads * p.splits;
-        p.part_floats = p.part_rows * c->head_dim;
+    const uint64_t rows = (uint64_t)max_q * share;
+    if (rows <= 32) {              // few rows everywhere
+        p.few = true;
+        p.few_rows = 0x7fffffff;
+        p.few_tiles = rows <= 16 ? 1 : 2;
+    } else {                       // many in some sequence; single tokens of others, if there may be any, in the other kernel
+        p.many = true;
+        p.few = share <= 32 && (uint64_t)b->n_seqs * max_q != b->n_tokens;
+        p.few_tiles = share <= 16 ? 1 : 2;
+        p.few_rows = p.few ? 16 * (int32_t)p.few_tiles : 0;
+    }
+    p.few_splits = p.many_splits = 1;
+    if (p.few) {                   // enough workgroups for four on each compute unit, of 128 keys at least
+        const uint64_t whole = (uint64_t)b->n_seqs * c->kv_heads, want = (4ull * cus + whole - 1) / whole, most = (max_kv + 127) / 128;
+        const uint64_t n = want < most ? want : most;
+        p.few_splits = (uint32_t)(n < 1 ? 1 : n > 256 ? 256 : n);
+        if (p.few_splits > 1) p.few_parts = whole * 16 * p.few_tiles * p.few_splits;
+    }
+    if (p.many) {                  // two on each compute unit, of 512 keys at least
+        p.many_tiles = (uint32_t)((uint64_t)b->n_tokens * share / MANY_ROWS) + b->n_seqs;
+        const uint64_t whole = (uint64_t)p.many_tiles * c->kv_heads, want = 2ull * cus / whole, most = (max_kv + 511) / 512;
+        const uint64_t n = want < most ? want : most;
+        p.many_splits = (uint32_t)(n < 1 ? 1 : n);
+        if (p.many_splits > 1) p.many_parts = (uint64_t)b->n_tokens * heads * p.many_splits;
     }
     return p;
 }
 
+uint64_t workspace_of(const Shape &p, uint32_t head_dim) { return (p.few_parts + p.many_parts) * (head_dim + 2) * 4; }
+
 int check_heads(const ecfa_cache *c, uint32_t heads)
 {
     return heads == 0 || heads > (1u << 20) || heads % c->kv_heads ? ECF8_E_ARG : ECF8_OK;
+}
+
+// Rows of a sequence are counted in 32 bits, and a launch's threads, 256 a workgroup, too.
+int check_counts(const ecfa_cache *c, const ecfa_batch *b, uint32_t heads, const Shape &p)
+{
+    if ((uint64_t)b->n_tokens * (heads / c->kv_heads) > (1u << 30)) return ECF8_E_ARG;
+    const uint64_t most = 0xffffff;
+    if (p.few && (uint64_t)b->n_seqs * c->kv_heads * p.few_splits > most) return ECF8_E_ARG;
+    if (p.many && (uint64_t)p.many_tiles * c->kv_heads * p.many_splits > most) return ECF8_E_ARG;
+    return p.few_parts / p.few_splits + p.many_parts / p.many_splits > most ? ECF8_E_ARG : ECF8_OK;
 }
 
 int check_attend_rows(const ecfa_rows *r, uint32_t n_tokens)
@@ -114,7 +154,7 @@ uint64_t ecfa_attend_workspace_bytes(const ecfa_cache *cache, const ecfa_batch *
     if (!cache || !batch || cache_view(cache, true, &c) || batch_view(cache, batch, true, &b) || check_heads(cache, heads) || !batch->n_tokens) return 0;
     const int cus = device_cus();
     const Shape p = shape_of(cache, batch, heads, cus > 0 ? (uint32_t)cus : 256u);
-    return (p.part_floats + 2 * p.part_rows) * 4;
+    return check_counts(cache, batch, heads, p) ? 0 : workspace_of(p, cache->head_dim);
 }
 
 int ecfa_attend(const ecfa_cache *cache, const ecfa_batch *batch, const ecfa_attend_opts *opts, const ecfa_rows *q, const ecfa_rows *out,
@@ -136,13 +176,15 @@ int ecfa_attend(const ecfa_cache *cache, const ecfa_batch *batch, const ecfa_att
     const int cus = device_cus();
     if (cus <= 0) return ECF8_E_HIP;
     const Shape p = shape_of(cache, batch, q->heads, (uint32_t)cus);
-    const uint64_t need = (p.part_floats + 2 * p.part_rows) * 4;
+    if ((rc = check_counts(cache, batch, q->heads, p))) return rc;
+    const uint64_t need = workspace_of(p, cache->head_dim);
     if (need) {
         if (!d_workspace) return ECF8_E_ARG;
         if ((uintptr_t)d_workspace & 15) return ECF8_E_ALIGN;
         if (workspace_bytes < need) return ECF8_E_CAPACITY;
         a.part = (float *)d_workspace;
-        a.part_ml = a.part + p.part_floats;
+        a.part_ml = a.part + (p.few_parts + p.many_parts) * cache->head_dim;
+        a.many_part0 = (int64_t)p.few_parts;
     }
     a.q = (const uint8_t *)q->d;
     a.out = (uint8_t *)out->d;
@@ -160,16 +202,18 @@ int ecfa_attend(const ecfa_cache *cache, const ecfa_batch *batch, const ecfa_att
     a.share = q->heads / cache->kv_heads;
     a.causal = opts->causal;
     a.window = opts->window;
-    a.splits = p.splits;
-    a.row_tiles = p.row_tiles;
-    a.tile_rows = p.tile_rows;
-    a.split_unit = p.split_unit;
+    a.few_rows = p.few_rows;
+    a.few_tile = 16 * p.few_tiles;
+    a.few_splits = p.few_splits;
+    a.many_tiles = p.many_tiles;
+    a.many_splits = p.many_splits;
     hipStream_t s = (hipStream_t)stream;
-    // a launch counts its threads, 256 a workgroup, in 32 bits
-    if ((uint64_t)batch->n_seqs * p.row_tiles * a.kv_heads * p.splits > 0xffffff || (p.splits > 1 && (uint64_t)batch->n_tokens * a.heads > 0xffffff)) return ECF8_E_ARG;
-    rc = cache->dtype == ECFA_E4M3 ? launch_few_rows_e4m3(a, p.kc, p.tiles, s) : launch_few_rows_bf16(a, p.kc, p.tiles, s);
-    if (rc || p.splits <= 1) return rc;
-    hipLaunchKernelGGL(ecfa_attend_join_kernel, dim3(batch->n_tokens * a.heads), dim3(JOIN_THREADS), 0, s, a);
+    const bool f8 = cache->dtype == ECFA_E4M3;
+    if (p.few) rc = f8 ? launch_few_rows_e4m3(a, p.kc, p.few_tiles, s) : launch_few_rows_bf16(a, p.kc, p.few_tiles, s);
+    if (p.many && !rc) rc = f8 ? launch_many_rows_e4m3(a, p.kc, s) : launch_many_rows_bf16(a, p.kc, s);
+    if (rc || !need) return rc;
+    const uint32_t few_blocks = (uint32_t)(p.few_parts / p.few_splits), blocks = few_blocks + (uint32_t)(p.many_parts / p.many_splits);
+    hipLaunchKernelGGL(ecfa_attend_join_kernel, dim3(blocks), dim3(JOIN_THREADS), 0, s, a, few_blocks);
     return hipGetLastError() == hipSuccess ? ECF8_OK : ECF8_E_HIP;
 }
 

@@ -9,19 +9,15 @@
 
 namespace ecfa {
 
-constexpr int FEW_WAVES = 4;
-
 template <int KC, bool F8, int NT>
 struct FewShape {
     static constexpr int E = F8 ? 1 : 2;
     static constexpr int ROW = KC * 32 * E, PAD = F8 ? 16 : 32;      // bytes; the pad spreads the rows that a transposing read touches over the banks
     static constexpr int STRIDE = ROW + PAD;
     static constexpr int V_BYTES = 32 * STRIDE;                      // of a wave
-    static constexpr int P_BYTES = 32 * 17 * 4;                      // weights of one step and 16 rows, for the slow way
-    static constexpr int WAVE_BYTES = V_BYTES > P_BYTES ? V_BYTES : P_BYTES;
     static constexpr int O_STRIDE = KC * 32 + 4;                     // floats
     static constexpr int JOIN_BYTES = FEW_WAVES * 16 * (O_STRIDE + 2) * 4;
-    static constexpr int MAIN_BYTES = FEW_WAVES * (V_BYTES + P_BYTES);
+    static constexpr int MAIN_BYTES = FEW_WAVES * V_BYTES;
     static constexpr int BYTES = MAIN_BYTES > JOIN_BYTES ? MAIN_BYTES : JOIN_BYTES;
 };
 
@@ -34,34 +30,31 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void ecfa_attend_few_kernel(cons
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int g = lane / 16, col = lane % 16;
     uint32_t at = blockIdx.x;
-    const uint32_t split = at % a.splits;
-    at /= a.splits;
-    const uint32_t kvh = at % a.kv_heads;
-    at /= a.kv_heads;
-    const uint32_t tile0 = at % a.row_tiles, s = at / a.row_tiles;
+    const uint32_t split = at % a.few_splits;
+    at /= a.few_splits;
+    const uint32_t kvh = at % a.kv_heads, s = at / a.kv_heads;
     const Seq sq = seq_of(a.b, s);
     const int32_t prefix = prefix_of(a, s, sq);
     const int32_t rows = sq.qn * (int32_t)a.share;
+    if (rows > a.few_rows) return;                             // the other kernel's
     const uint8_t *k0 = a.c.k + (int64_t)kvh * a.c.k_head, *v0 = a.c.v + (int64_t)kvh * a.c.v_head;
     const int32_t *table = a.b.table + (int64_t)s * a.b.table_stride;
     const uint32_t in_page = (1u << a.c.page_shift) - 1;
     const float k_scale = a.c.k_scale ? a.c.k_scale[kvh] : 1.f, v_scale = a.c.v_scale ? a.c.v_scale[kvh] : 1.f;
     const float to_log2 = a.scale_log2 * k_scale;
-    uint8_t *my_v = lds + wave * (S::V_BYTES + S::P_BYTES);
-    float *my_p = (float *)(my_v + S::V_BYTES);
+    uint8_t *my_v = lds + wave * S::V_BYTES;
 
-    // max_q is a hint: if a sequence has more rows than the grid covers, a workgroup takes several tiles
-    for (int32_t row0 = (int32_t)tile0 * 16 * NT; row0 < rows; row0 += (int32_t)a.row_tiles * 16 * NT) {
+    // max_q is a hint: if a sequence has more rows than a tile after all, the tiles follow one another
+    for (int32_t row0 = 0; row0 < rows; row0 += 16 * NT) {
         const int32_t row_end = row0 + 16 * NT < rows ? row0 + 16 * NT : rows;
         const int32_t tok_a = row0 / (int32_t)a.share, tok_b = (row_end - 1) / (int32_t)a.share;
         const KeyRange kr = keys_of(a, sq, prefix, tok_a, tok_b);
-        const Split sp = split_of(kr, a.splits, (int32_t)a.split_unit);
+        const Split sp = split_of(kr, row0 == 0 ? a.few_splits : 1, FEW_UNIT);
         const bool alone = sp.used <= 1;
         if ((int32_t)split >= (sp.used > 1 ? sp.used : 1)) continue;
 
         // this lane's rows, one of each sub-tile
         int64_t o_at[NT];
-        int64_t part_row[NT];
         int32_t lo[NT], hi[NT], place[NT];
         float slope[NT];
         bf16x8 q[NT][KC];
@@ -73,7 +66,6 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void ecfa_attend_few_kernel(cons
             const uint32_t head = kvh * a.share + (there ? (uint32_t)r % a.share : 0);
             const int64_t t = sq.q0 + tok;
             o_at[n] = t * a.o_tok + (int64_t)head * a.o_head;
-            part_row[n] = t * a.heads + head;
             place[n] = sq.place0 + tok;
             slope[n] = a.slopes ? a.slopes[head] * LOG2E : 0.f;
             const KeyRange own = keys_of(a, sq, prefix, tok, tok);
@@ -91,6 +83,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void ecfa_attend_few_kernel(cons
 
         f32x4 o[NT][2 * KC];
         float m[NT], l[NT];
+        int poison = 0;
 #pragma unroll
         for (int n = 0; n < NT; n++) {
             m[n] = NONE;
@@ -191,7 +184,6 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void ecfa_attend_few_kernel(cons
             pages_of(step + 2 * FEW_WAVES, page_next, ok_next);
 
             bf16x8 p[NT];
-            uint32_t seen[NT];                                 // of this row: bit of each key (where the step is not whole)
 #pragma unroll
             for (int n = 0; n < NT; n++) {
 #pragma unroll
@@ -207,13 +199,11 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void ecfa_attend_few_kernel(cons
                             const int32_t far = place[n] - (key0 + 16 * u + 4 * g + i);
                             x[n][u][i] -= slope[n] * (float)(far < 0 ? -far : far);
                         }
-                seen[n] = 0xffffffffu;
                 if (!whole) {
                     const int32_t below = lo[n] - key0, above = hi[n] - key0;      // bits [below, above)
                     uint32_t bits = ok_now;
                     bits &= above >= 32 ? 0xffffffffu : above <= 0 ? 0u : (1u << above) - 1;
                     bits &= below <= 0 ? 0xffffffffu : below >= 32 ? 0u : ~((1u << below) - 1);
-                    seen[n] = bits;
                     for (int u = 0; u < 2; u++)
                         for (int i = 0; i < 4; i++)
                             if (!(bits >> (16 * u + 4 * g + i) & 1)) x[n][u][i] = NONE;
@@ -241,7 +231,6 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void ecfa_attend_few_kernel(cons
 
             // O^T += V^T P^T
             const bool apart = !whole && tok_b > tok_a;        // rows that see different keys of this step
-            bool poison = false;
 #pragma unroll
             for (int d = 0; d < 2 * KC; d++) {
                 bf16x8 vf;
@@ -260,59 +249,33 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void ecfa_attend_few_kernel(cons
                 if (apart) {                                   // 0 * v is 0 unless v is NaN or infinite
                     const bf16x8 zero = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
                     const f32x4 z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, zero, f32x4{0, 0, 0, 0}, 0, 0, 0);
-                    poison = poison || !(z[0] == 0.f && z[1] == 0.f && z[2] == 0.f && z[3] == 0.f);
+                    for (int i = 0; i < 4; i++) poison |= z[i] != 0.f ? 1 : 0;
                 }
 #pragma unroll
-                for (int n = 0; n < NT; n++)
-                    if (!apart) o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[n], o[n][d], 0, 0, 0);
+                for (int n = 0; n < NT; n++) o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[n], o[n][d], 0, 0, 0);
             }
-            if (apart) {
-                if (!__any(poison)) {
+        }
+        if (__any(poison)) {                                   // this wave's keys once more, for all its rows
 #pragma unroll
-                    for (int d = 0; d < 2 * KC; d++) {
-                        bf16x8 vf;
-                        if constexpr (F8) {
-                            typedef __attribute__((ext_vector_type(2))) int i32x2;
-                            const int row = (col / 2 < 4 ? 0 : 12) + 4 * g + col / 2;
-                            const auto src = (__attribute__((address_space(3))) i32x2 *)(my_v + row * S::STRIDE + 16 * d + 8 * (col & 1));
-                            const i32x2 y = __builtin_amdgcn_ds_read_tr8_b64_v2i32(src);
-                            vf = bf16_of_e4m3((uint32_t)y[0], (uint32_t)y[1]);
-                        } else {
-                            const uint8_t *src = my_v + (4 * g + col / 4) * S::STRIDE + 32 * d + 8 * (col % 4);
-                            const bf16x4 y0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4 *)src);
-                            const bf16x4 y1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4 *)(src + 16 * S::STRIDE));
-                            vf = bf16x8{y0[0], y0[1], y0[2], y0[3], y1[0], y1[1], y1[2], y1[3]};
-                        }
-#pragma unroll
-                        for (int n = 0; n < NT; n++) o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[n], o[n][d], 0, 0, 0);
-                    }
-                } else {                                       // key by key, and only for the rows that see the key
-#pragma unroll
-                    for (int n = 0; n < NT; n++) {
-                        lds_fence_wave();
-                        for (int u = 0; u < 2; u++)
-                            for (int i = 0; i < 4; i++) my_p[(16 * u + 4 * g + i) * 17 + col] = (float)p[n][4 * u + i];
-                        lds_fence_wave();
-                        for (int key = 0; key < 32; key++) {
-                            const float w = my_p[key * 17 + col];
-                            const bool use = seen[n] >> key & 1;
-#pragma unroll
-                            for (int d = 0; d < 2 * KC; d++) {
-                                const uint8_t *src = my_v + key * S::STRIDE + (16 * d + 4 * g) * E;
-                                float v[4];
-                                if constexpr (F8) {
-                                    const uint32_t y = *(const uint32_t *)src;
-                                    const bf16x8 f = bf16_of_e4m3(y, 0);
-                                    for (int i = 0; i < 4; i++) v[i] = (float)f[i];
-                                } else {
-                                    const bf16x4 f = *(const bf16x4 *)src;
-                                    for (int i = 0; i < 4; i++) v[i] = (float)f[i];
-                                }
-                                for (int i = 0; i < 4; i++) o[n][d][i] = use ? o[n][d][i] + w * v[i] : o[n][d][i];
-                            }
-                        }
-                    }
+            for (int n = 0; n < NT; n++) {
+                const KeyRange own{lo[n], hi[n], 0, 0};
+                float y[8 * KC], m_slow = NONE, l_slow = 0.f;
+                const int32_t r = row0 + 16 * n + col < row_end ? row0 + 16 * n + col : row0;
+                const uint8_t *src = a.q + (sq.q0 + r / (int32_t)a.share) * a.q_tok + (int64_t)(kvh * a.share + (uint32_t)r % a.share) * a.q_head;
+                for (int32_t st = step_a + wave; st < step_b; st += FEW_WAVES) {
+                    float z[8 * KC], m_step, l_step;
+                    attend_slowly<F8, 4, 2 * KC>(a, src, k0, v0, table, st, st + 1, own, place[n], to_log2, slope[n], g, [&](int i) { return 16 * i + 4 * g; }, z,
+                                                 m_step, l_step);
+                    const float m_new = max_f(m_slow, m_step), base = m_new == NONE ? 0.f : m_new;
+                    const float f0 = exp2_fast(m_slow - base), f1 = exp2_fast(m_step - base);
+                    for (int i = 0; i < 8 * KC; i++) y[i] = st == step_a + wave ? z[i] : y[i] * f0 + z[i] * f1;
+                    l_slow = l_slow * f0 + l_step * f1;
+                    m_slow = m_new;
                 }
+                m[n] = m_slow;
+                l[n] = g == 0 ? l_slow : 0.f;                  // the lanes of a row each have the whole sum
+#pragma unroll
+                for (int d = 0; d < 2 * KC; d++) o[n][d] = f32x4{y[4 * d], y[4 * d + 1], y[4 * d + 2], y[4 * d + 3]};
             }
         }
 
@@ -337,7 +300,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void ecfa_attend_few_kernel(cons
                 all += lj[w * 16 + r] * share[w];
             }
             const int64_t o_row = __shfl(o_at[n], r & 15);     // lane r % 16 of this wave holds row r
-            const int64_t p_row = __shfl(part_row[n], r & 15);
+            const int64_t part = few_part(a, s, kvh, 16 * n + r) + split;      // of the first tile: the others are not split
             if (row0 + 16 * n + r < row_end) {
                 for (int d = 4 * e; d < (int)a.head_dim; d += 64) {
                     f32x4 y{0, 0, 0, 0};
@@ -349,11 +312,11 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void ecfa_attend_few_kernel(cons
                         *(bf16x4 *)(a.out + o_row + 2 * d) = z;
                     } else {
                         for (int i = 0; i < 4; i++) y[i] *= v_scale;
-                        *(f32x4 *)(a.part + (p_row * a.splits + split) * a.head_dim + d) = y;
+                        *(f32x4 *)(a.part + part * a.head_dim + d) = y;
                     }
                 }
                 if (!alone && e == 0) {
-                    float *ml = a.part_ml + (p_row * a.splits + split) * 2;
+                    float *ml = a.part_ml + part * 2;
                     ml[0] = top;
                     ml[1] = all;
                 }
@@ -366,7 +329,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void ecfa_attend_few_kernel(cons
 template <int KC, bool F8>
 int launch_few_rows_kc(const AttendArgs &a, uint32_t tiles, hipStream_t s)
 {
-    const uint64_t grid = (uint64_t)a.b.n_seqs * a.row_tiles * a.kv_heads * a.splits;
+    const uint64_t grid = (uint64_t)a.b.n_seqs * a.kv_heads * a.few_splits;
     if (tiles == 1) hipLaunchKernelGGL((ecfa_attend_few_kernel<KC, F8, 1>), dim3((unsigned)grid), dim3(FEW_WAVES * 64), 0, s, a);
     else hipLaunchKernelGGL((ecfa_attend_few_kernel<KC, F8, 2>), dim3((unsigned)grid), dim3(FEW_WAVES * 64), 0, s, a);
     return hipGetLastError() == hipSuccess ? ECF8_OK : ECF8_E_HIP;

@@ -1,0 +1,379 @@
+// Attention for sequences with many rows (prompts, chunks of them): bound by the matrix cores and the softmax beside them.
+//
+// A workgroup takes one (tile of 128 rows, key/value head, split of the keys); each of its four waves holds 32 rows, their Q and their
+// O, and all of them walk over the same 64 keys at a time, whose K and V lie in LDS as BF16 (two buffers: the next 64 keys arrive
+// while the present ones are worked on, one barrier a step).  BF16 goes from memory to LDS without touching registers, E4M3 is turned into BF16
+// on the way, once for the four waves.  The 16-byte pieces of a row are permuted by the row's number, so that neither the reads
+// of K (16 rows, one piece) nor the transposing reads of V (4 rows, two pieces) meet in a bank.
+#pragma once
+#include "ecfa_attend.h"
+
+namespace ecfa {
+
+template <int KC>
+struct ManyShape {
+    static constexpr int ROW = KC <= 2 ? 128 : KC <= 4 ? 256 : 512;   // bytes of a key's row in LDS
+    static constexpr int PIECES = ROW / 16;
+    static constexpr int TILE = MANY_KEYS * ROW;                      // K or V
+    static constexpr int BYTES = 4 * TILE;
+};
+
+// Which piece of a row stands where: piece p of row r at place p ^ spread(r).
+template <int KC>
+__device__ inline int spread(int r)
+{
+    return KC <= 2 ? (r >> 1 & 1) << 2 | (r >> 2 & 3) : (r & 3) << 2 | (r >> 2 & 3);
+}
+
+// The first tile of a sequence among all tiles of the launch: rows before it, in whole tiles, and one more for each sequence before it,
+// which is never less than they need.
+__device__ inline uint32_t first_tile(const AttendArgs &a, uint32_t s)
+{
+    int32_t x = a.b.q_start ? a.b.q_start[s] : (int32_t)s;
+    x = x < 0 ? 0 : x > (int32_t)a.b.n_tokens ? (int32_t)a.b.n_tokens : x;
+    return (uint32_t)((uint64_t)x * a.share / MANY_ROWS) + s;
+}
+
+__device__ inline uint32_t seq_of_tile(const AttendArgs &a, uint32_t tile)     // as seq_of_row
+{
+    uint32_t lo = 0, n = a.b.n_seqs;
+    while (n > 1) {
+        const uint32_t step = (n + 63) / 64, i = (threadIdx.x & 63) * step;
+        const uint64_t hit = __ballot(i < n && first_tile(a, lo + i) <= tile);
+        const uint32_t c = hit ? 64 - __clzll((long long)hit) : 1;
+        const uint32_t skip = (c - 1) * step;
+        lo += skip;
+        n = n - skip < step ? n - skip : step;
+    }
+    return lo;
+}
+
+template <int KC, bool F8, bool EXTRA>
+__global__ __launch_bounds__(MANY_WAVES * 64, KC <= 4 ? 2 : 1) void ecfa_attend_many_kernel(const AttendArgs a)
+{
+    using S = ManyShape<KC>;
+    typedef __attribute__((address_space(3))) uint8_t lds_u8;
+    typedef __attribute__((address_space(1))) const uint8_t hbm_u8;
+    constexpr int NC = 2 * KC;                                 // pieces of 16 elements along a head
+    __shared__ __align__(16) uint8_t lds[S::BYTES];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int half = lane / 32, col = lane % 32;
+    // heads of keys next to each other in launch order: workgroups with the same keys then land on the same XCD where the heads
+    // are a multiple of eight.  The last tiles, which see the most keys, go first.
+    const uint32_t kvh = blockIdx.x % a.kv_heads;
+    uint32_t at = blockIdx.x / a.kv_heads;
+    const uint32_t split = at % a.many_splits;
+    at = a.many_tiles - 1 - at / a.many_splits;
+    const uint32_t s = seq_of_tile(a, at);
+    const Seq sq = seq_of(a.b, s);
+    const int32_t rows = sq.qn * (int32_t)a.share;
+    if (rows <= a.few_rows) return;                            // the other kernel's
+    const int32_t row0 = (int32_t)(at - first_tile(a, s)) * MANY_ROWS;
+    if (row0 >= rows) return;
+    const int32_t row_end = row0 + MANY_ROWS < rows ? row0 + MANY_ROWS : rows;
+    const int32_t prefix = prefix_of(a, s, sq);
+    const int32_t share = (int32_t)a.share;
+    const int32_t tok_a = row0 / share, tok_b = (row_end - 1) / share;
+    const KeyRange kr = keys_of(a, sq, prefix, tok_a, tok_b);
+    const Split sp = split_of(kr, a.many_splits, MANY_UNIT);
+    const bool alone = sp.used <= 1;
+    if ((int32_t)split >= (sp.used > 1 ? sp.used : 1)) return;
+
+    const uint8_t *k0 = a.c.k + (int64_t)kvh * a.c.k_head, *v0 = a.c.v + (int64_t)kvh * a.c.v_head;
+    const int32_t *table = a.b.table + (int64_t)s * a.b.table_stride;
+    const uint32_t in_page = (1u << a.c.page_shift) - 1;
+    const float k_scale = a.c.k_scale ? a.c.k_scale[kvh] : 1.f, v_scale = a.c.v_scale ? a.c.v_scale[kvh] : 1.f;
+    const float to_log2 = a.scale_log2 * k_scale;
+
+    // this lane's row
+    const int32_t r = row0 + 32 * wave + col;
+    const bool there = r < row_end;
+    const int32_t tok = there ? r / share : tok_a;
+    const uint32_t head = kvh * a.share + (there ? (uint32_t)(r % share) : 0u);
+    const int64_t t = sq.q0 + tok;
+    const int32_t place = sq.place0 + tok;
+    const float slope = EXTRA && a.slopes ? a.slopes[head] * LOG2E : 0.f;
+    const KeyRange own = keys_of(a, sq, prefix, tok, tok);
+    bf16x8 q[NC];
+#pragma unroll
+    for (int c = 0; c < NC; c++) {
+        const int d = 16 * c + 8 * half;
+        u32x4 x{0, 0, 0, 0};
+        if (there && d < (int)a.head_dim) x = *(const u32x4 *)(a.q + t * a.q_tok + (int64_t)head * a.q_head + 2 * d);
+        q[c] = __builtin_bit_cast(bf16x8, x);
+    }
+    f32x16 o[KC];
+#pragma unroll
+    for (int d = 0; d < KC; d++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) o[d][i] = 0.f;
+    float m = NONE, l = 0.f;
+    int poison = 0;
+
+    if (a.head_dim < KC * 32 || KC == 3 || KC == 6) {          // what no load fills: zeros, for the products of elements past a head's end
+        for (int i = threadIdx.x * 16; i < 4 * S::TILE; i += MANY_WAVES * 64 * 16) *(u32x4 *)(lds + i) = u32x4{0, 0, 0, 0};
+        __syncthreads();
+    }
+
+    const int32_t step_a = sp.first + (int32_t)split * sp.per;
+    const int32_t step_b = step_a + sp.per < sp.first + sp.count ? step_a + sp.per : sp.first + sp.count;
+
+    // The page of key 32 * step + lane as the table has it.  It is looked at a step later, so that nothing waits for the table.
+    const auto entry_of = [&](int32_t step) {
+        const int32_t key = 32 * step + lane;
+        uint32_t e = 0xffffffffu;
+        if (step < step_b && key < sq.len) e = (uint32_t)table[(uint32_t)key >> a.c.page_shift];
+        return e;
+    };
+    // Of each of the 64 keys, whether any row of the tile may look at it
+    const auto seen_by_some = [&](int32_t step, uint32_t e) {
+        const int32_t key = 32 * step + lane;
+        return (uint64_t)__ballot(e < a.c.n_pages && key >= kr.lo && key < kr.hi);
+    };
+    // This wave's 16 of the 64 keys, from memory to LDS.  Pages of 16 tokens and more hold them together (the first of them is in the
+    // table if any is), and then their place is worked out by the scalar unit; smaller ones are looked up row by row.
+    constexpr int LOAD_PIECES = F8 ? S::ROW / 32 : S::PIECES;  // 16-byte pieces of a row in memory
+    constexpr int PER = 64 / LOAD_PIECES, LOADS = 16 / PER;    // rows of a load, loads
+    const int load_row = lane / LOAD_PIECES, load_piece = lane % LOAD_PIECES;
+    u32x4 kx[F8 ? LOADS : 1], vx[F8 ? LOADS : 1];
+    const auto fetch_rows = [&](int n, const uint8_t *ks, const uint8_t *vs, uint64_t ok, int buffer) {
+        const int row = 16 * wave + PER * n + load_row;
+        if constexpr (F8) {
+            const int off = 16 * load_piece < (int)a.head_dim ? 16 * load_piece : 0;
+            kx[n] = *(const u32x4 *)(ks + off);
+            vx[n] = *(const u32x4 *)(vs + off);
+            if (ok != ~0ull && !(ok >> row & 1)) vx[n] = u32x4{0, 0, 0, 0};
+        } else {
+            const int off = 16 * (load_piece ^ spread<KC>(row & 15));
+            uint8_t *dst = lds + buffer * 2 * S::TILE + (16 * wave + PER * n) * S::ROW;
+            if (off < 2 * (int)a.head_dim) {
+                __builtin_amdgcn_global_load_lds((hbm_u8 *)(ks + off), (lds_u8 *)dst, 16, 0, 0);
+                if (ok == ~0ull || (ok >> row & 1)) __builtin_amdgcn_global_load_lds((hbm_u8 *)(vs + off), (lds_u8 *)(dst + S::TILE), 16, 0, 0);
+                else *(u32x4 *)(dst + S::TILE + lane * 16) = u32x4{0, 0, 0, 0};
+            }
+        }
+    };
+    const int64_t k_lane = (int64_t)load_row * a.c.k_tok, v_lane = (int64_t)load_row * a.c.v_tok;
+    const auto fetch = [&](int32_t step, uint32_t e, uint64_t ok, int buffer) {
+        if (a.c.page_shift >= 4) {
+            const uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)e, 16 * wave);
+            const int64_t pg = first < a.c.n_pages ? first : 0u, in = (uint32_t)(32 * step + 16 * wave) & in_page;
+            const uint8_t *ks = k0 + pg * a.c.k_page + in * a.c.k_tok, *vs = v0 + pg * a.c.v_page + in * a.c.v_tok;
+#pragma unroll
+            for (int n = 0; n < LOADS; n++) fetch_rows(n, ks + n * PER * a.c.k_tok + k_lane, vs + n * PER * a.c.v_tok + v_lane, ok, buffer);
+        } else {
+#pragma unroll
+            for (int n = 0; n < LOADS; n++) {
+                const int row = 16 * wave + PER * n + load_row;
+                const uint32_t mine = (uint32_t)__shfl((int)e, row);
+                const int64_t pg = mine < a.c.n_pages ? mine : 0u, in = (uint32_t)(32 * step + row) & in_page;
+                fetch_rows(n, k0 + pg * a.c.k_page + in * a.c.k_tok, v0 + pg * a.c.v_page + in * a.c.v_tok, ok, buffer);
+            }
+        }
+    };
+    const auto store = [&](int buffer) {
+        if constexpr (F8) {
+#pragma unroll
+            for (int n = 0; n < LOADS; n++) {
+                const int row = 16 * wave + PER * n + load_row, piece = load_piece;
+                if (16 * piece < (int)a.head_dim) {
+                    uint8_t *dst = lds + buffer * 2 * S::TILE + row * S::ROW;
+                    const int p0 = (2 * piece ^ spread<KC>(row & 15)) * 16, p1 = ((2 * piece + 1) ^ spread<KC>(row & 15)) * 16;
+                    *(bf16x8 *)(dst + p0) = bf16_of_e4m3(kx[n][0], kx[n][1]);
+                    *(bf16x8 *)(dst + p1) = bf16_of_e4m3(kx[n][2], kx[n][3]);
+                    *(bf16x8 *)(dst + S::TILE + p0) = bf16_of_e4m3(vx[n][0], vx[n][1]);
+                    *(bf16x8 *)(dst + S::TILE + p1) = bf16_of_e4m3(vx[n][2], vx[n][3]);
+                }
+            }
+        }
+    };
+
+    // where this lane reads K and V: bytes from the start of a tile; chunks of a head by exclusive or, keys by addition
+    const int k_at = col * S::ROW + ((half ^ spread<KC>(col & 15)) << 4);
+    const int vr = 4 * half + lane % 16 / 4, vp = 2 * (lane / 16 % 2) + lane % 4 / 2;
+    const int v_at = vr * S::ROW + ((vp ^ spread<KC>(vr)) << 4) + 8 * (lane & 1);
+    const int v_at8 = (vr + 8) * S::ROW + ((vp ^ spread<KC>(vr + 8)) << 4) + 8 * (lane & 1);
+    typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
+    typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
+    // Eight keys of V: of 16 that begin at `keys`, elements 32 d .. of the head; `y0`, `y1`: this lane's places in the first 16 keys
+    const auto v_frag = [&](int y0, int y1, int d, int keys) {
+        const bf16x4 a0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(uintptr_t)(uint32_t)((y0 ^ d << 6) + keys * S::ROW));
+        const bf16x4 a1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(uintptr_t)(uint32_t)((y1 ^ d << 6) + keys * S::ROW));
+        return bf16x8{a0[0], a0[1], a0[2], a0[3], a1[0], a1[1], a1[2], a1[3]};
+    };
+    const int lds0 = (int)(uint32_t)(uintptr_t)(lds_u8 *)lds;
+
+    uint32_t entry = entry_of(step_a);
+    uint64_t ok = seen_by_some(step_a, entry);
+    if (step_a < step_b) fetch(step_a, entry, ok, 0);
+    store(0);
+    entry = entry_of(step_a + 2);
+    int buffer = 0;
+    for (int32_t step = step_a; step < step_b; step += 2) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // loads into LDS are no loads to the barrier's own wait
+        __syncthreads();                                       // this step's keys are here, and nobody reads the other buffer any more
+        const uint64_t ok_now = ok;
+        ok = seen_by_some(step + 2, entry);
+        if (step + 2 < step_b) fetch(step + 2, entry, ok, buffer ^ 1);
+        entry = entry_of(step + 4);
+        // Made anew each step, from three registers instead of kept in sixteen
+        int ka = lds0 + buffer * 2 * S::TILE + k_at, va = lds0 + buffer * 2 * S::TILE + S::TILE + v_at, va8 = lds0 + buffer * 2 * S::TILE + S::TILE + v_at8;
+        asm volatile("" : "+v"(ka), "+v"(va), "+v"(va8));
+        f32x16 x[2];
+#pragma unroll
+        for (int u = 0; u < 2; u++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) x[u][i] = 0.f;
+#pragma unroll
+        for (int c = 0; c < NC; c++)
+#pragma unroll
+            for (int u = 0; u < 2; u++) {
+                const bf16x8 kf = *(lds_bf16x8 *)(uintptr_t)(uint32_t)((ka ^ c << 5) + u * 32 * S::ROW);
+                x[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[c], x[u], 0, 0, 0);
+            }
+        const int32_t key0 = 32 * step;
+        const bool whole = ok_now == ~0ull && key0 >= kr.full_lo && key0 + 64 <= kr.full_hi;
+        // x[u][i]: row `col`, key 32 u + 8 (i / 4) + 4 half + i % 4
+        float c_log2 = to_log2;
+        if constexpr (EXTRA) {
+            c_log2 = 1.f;
+#pragma unroll
+            for (int u = 0; u < 2; u++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) {
+                    float y = x[u][i] * to_log2;
+                    if (a.cap > 0.f) y = capped(y, a.cap);
+                    const int32_t far = place - (key0 + 32 * u + 8 * (i / 4) + 4 * half + i % 4);
+                    y -= slope * (float)(far < 0 ? -far : far);
+                    x[u][i] = y;
+                }
+        }
+        uint64_t seen = ~0ull;
+        if (!whole) {
+            const int32_t below = own.lo - key0, above = own.hi - key0;
+            seen = ok_now;
+            seen &= above >= 64 ? ~0ull : above <= 0 ? 0ull : (1ull << above) - 1;
+            seen &= below <= 0 ? ~0ull : below >= 64 ? 0ull : ~((1ull << below) - 1);
+            const uint32_t s0 = (uint32_t)seen >> (4 * half), s1 = (uint32_t)(seen >> 32) >> (4 * half);
+#pragma unroll
+            for (int i = 0; i < 16; i++) {
+                const uint32_t bit = 1u << (8 * (i / 4) + i % 4);
+                if (!(s0 & bit)) x[0][i] = NONE;
+                if (!(s1 & bit)) x[1][i] = NONE;
+            }
+        }
+        float top = NONE;
+#pragma unroll
+        for (int u = 0; u < 2; u++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) top = max_f(top, x[u][i]);
+        top = max_xor<32>(top) * c_log2;
+        // The maximum follows only where a score has outgrown it by 2^8: weights up to there lose nothing in BF16 or in the sums
+        if (__any(top > m + 8.f)) {
+            const float m_new = max_f(m, top);
+            const float shrink = exp2_fast(m - (m_new == NONE ? 0.f : m_new));
+            m = m_new;
+            l *= shrink;
+#pragma unroll
+            for (int d = 0; d < KC; d++)
+                o[d] *= shrink;
+        }
+        const float base = m == NONE ? 0.f : m;
+        u32x4 pw[4];
+        float l0 = 0.f, l1 = 0.f;
+        const bf16x2 ones{(__bf16)1.f, (__bf16)1.f};
+#pragma unroll
+        for (int u = 0; u < 2; u++)
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                const bf16x2 w = bf16_pair(exp2_fast(__builtin_fmaf(x[u][i], c_log2, -base)), exp2_fast(__builtin_fmaf(x[u][i + 1], c_log2, -base)));
+                pw[2 * u + i / 8][i % 8 / 2] = __builtin_bit_cast(uint32_t, w);
+                if (i % 4) l1 = __builtin_amdgcn_fdot2_f32_bf16(w, ones, l1, false);
+                else l0 = __builtin_amdgcn_fdot2_f32_bf16(w, ones, l0, false);
+            }
+        l += l0 + l1;
+        bf16x8 p[4];
+#pragma unroll
+        for (int n = 0; n < 4; n++) p[n] = __builtin_bit_cast(bf16x8, pw[n]);
+
+        if (!whole && tok_b > tok_a) {                         // rows that see different keys: 0 * v is 0 unless v is NaN or infinite
+            const bf16x8 zero = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
+            f32x16 z;
+            for (int i = 0; i < 16; i++) z[i] = 0.f;
+#pragma unroll
+            for (int d = 0; d < KC; d++)
+#pragma unroll
+                for (int n = 0; n < 4; n++) z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(va, va8, d, 16 * n), zero, z, 0, 0, 0);
+            for (int i = 0; i < 16; i++) poison |= z[i] != 0.f ? 1 : 0;
+        }
+#pragma unroll
+        for (int n = 0; n < 4; n++)
+#pragma unroll
+            for (int d = 0; d < KC; d++) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(va, va8, d, 16 * n), p[n], o[d], 0, 0, 0);
+        store(buffer ^ 1);
+        buffer ^= 1;
+    }
+
+    float all = sum_xor<32>(l);
+    if (__any(poison)) {
+        float y[16 * KC];
+        attend_slowly<F8, 2, 4 * KC>(a, a.q + t * a.q_tok + (int64_t)head * a.q_head, k0, v0, table, step_a, step_b, own, place, to_log2, slope, half,
+                                     [&](int n) { return 8 * n + 4 * half; }, y, m, all);
+#pragma unroll
+        for (int d = 0; d < KC; d++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) o[d][i] = y[16 * d + i];
+    }
+    if (!there) return;
+    if (alone) {
+        const float inv = all == 0.f ? 0.f : v_scale / all;
+        uint8_t *dst = a.out + t * a.o_tok + (int64_t)head * a.o_head;
+#pragma unroll
+        for (int d = 0; d < KC; d++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const int e = 32 * d + 8 * j + 4 * half;
+                bf16x4 y;
+                for (int i = 0; i < 4; i++) y[i] = (__bf16)(all == 0.f ? 0.f : o[d][4 * j + i] * inv);
+                if (e < (int)a.head_dim) *(bf16x4 *)(dst + 2 * e) = y;
+            }
+    } else {
+        const int64_t part = many_part(a, t, head) + split;
+#pragma unroll
+        for (int d = 0; d < KC; d++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const int e = 32 * d + 8 * j + 4 * half;
+                f32x4 y;
+                for (int i = 0; i < 4; i++) y[i] = o[d][4 * j + i] * v_scale;
+                if (e < (int)a.head_dim) *(f32x4 *)(a.part + part * a.head_dim + e) = y;
+            }
+        if (half == 0) {
+            a.part_ml[2 * part] = m;
+            a.part_ml[2 * part + 1] = all;
+        }
+    }
+}
+
+template <int KC, bool F8>
+int launch_many_rows_kc(const AttendArgs &a, hipStream_t s)
+{
+    const uint64_t grid = (uint64_t)a.many_tiles * a.kv_heads * a.many_splits;
+    if (a.cap > 0.f || a.slopes) hipLaunchKernelGGL((ecfa_attend_many_kernel<KC, F8, true>), dim3((unsigned)grid), dim3(MANY_WAVES * 64), 0, s, a);
+    else hipLaunchKernelGGL((ecfa_attend_many_kernel<KC, F8, false>), dim3((unsigned)grid), dim3(MANY_WAVES * 64), 0, s, a);
+    return hipGetLastError() == hipSuccess ? ECF8_OK : ECF8_E_HIP;
+}
+
+template <bool F8>
+int launch_many_rows(const AttendArgs &a, uint32_t kc, hipStream_t s)
+{
+    switch (kc) {
+    case 2: return launch_many_rows_kc<2, F8>(a, s);
+    case 3: return launch_many_rows_kc<3, F8>(a, s);
+    case 4: return launch_many_rows_kc<4, F8>(a, s);
+    case 6: return launch_many_rows_kc<6, F8>(a, s);
+    default: return launch_many_rows_kc<8, F8>(a, s);
+    }
+}
+
+} // namespace ecfa
