@@ -10,67 +10,81 @@ using namespace ecfa;
 
 constexpr int JOIN_THREADS = 256;
 
-// One workgroup for a (token, query head): the splits' (m, l, O) to one row.  The splits are dealt to groups of head_dim / 4 threads, so
-// that all partial rows are on their way at once.  Reads what the splits have written, 4 head_dim + 8 bytes each, once.
-// The first few_blocks workgroups are for the rows of the few-rows kernel's first tiles, the others for tokens of the other kernel.
-__global__ __launch_bounds__(JOIN_THREADS) void ecfa_attend_join_kernel(const AttendArgs a, uint32_t few_blocks)
+// One workgroup for a (token, query head): the pieces' (m, l, O) to one row.  They are dealt to groups of head_dim / 4 threads, so
+// that all partial rows are on their way at once.  Reads what the pieces have written, 4 head_dim + 8 bytes each, once.
+// The first few_blocks workgroups are for the rows of the few-rows kernel's first tiles (few_joined of each sequence and key/value head
+// next to each other, and what lies beyond those in turn), the others for tokens of the other kernel.
+__global__ __launch_bounds__(JOIN_THREADS) void ecfa_attend_join_kernel(const AttendArgs a, uint32_t few_blocks, uint32_t few_joined)
 {
     __shared__ f32x4 sums[JOIN_THREADS];
     __shared__ float alls[JOIN_THREADS];
-    const bool few = blockIdx.x < few_blocks;
-    uint32_t at = few ? blockIdx.x : blockIdx.x - few_blocks, s, head;
-    int32_t row, tile;                                         // of the sequence and its key/value head
-    if (few) {
-        row = (int32_t)(at % a.few_tile);
-        at /= a.few_tile;
-        s = at / a.kv_heads;
-        head = at % a.kv_heads * a.share + (uint32_t)row % a.share;
-        tile = (int32_t)a.few_tile;
+    const int32_t share = (int32_t)a.share;
+    int32_t row, used, rows, by;                               // row of the sequence and its key/value head
+    int64_t part, stride;                                      // its first partial row, and how far they lie apart
+    uint32_t kvh;
+    Seq sq;
+    if (blockIdx.x < few_blocks) {
+        row = (int32_t)(blockIdx.x % few_joined);
+        kvh = blockIdx.x / few_joined % a.kv_heads;
+        const uint32_t s = blockIdx.x / few_joined / a.kv_heads;
+        const FewItem it = few_plan(a, s, true);
+        if (!it.there || it.used <= 1) return;                 // not this kernel's, or written already
+        sq = seq_of(a.b, s);
+        rows = sq.qn * share;
+        rows = rows < (int32_t)a.few_tile ? rows : (int32_t)a.few_tile;
+        by = (int32_t)few_joined;
+        used = it.used;
+        part = few_part(a, it.first_item, kvh, 0);
+        stride = (int64_t)a.kv_heads * a.few_tile;
     } else {
-        head = at % a.heads;
-        s = seq_of_row(a.b, at / a.heads);
-        tile = MANY_ROWS;
-    }
-    const Seq sq = seq_of(a.b, s);
-    const int32_t share = (int32_t)a.share, rows = sq.qn * share;
-    if (!few) {
-        const int32_t tok = (int32_t)(at / a.heads) - sq.q0;
-        if (tok < 0 || tok >= sq.qn) return;
+        const uint32_t at = blockIdx.x - few_blocks, t = at / a.heads, head = at % a.heads, s = seq_of_row(a.b, t);
+        sq = seq_of(a.b, s);
+        const int32_t tok = (int32_t)t - sq.q0;
+        rows = sq.qn * share;
+        if (tok < 0 || tok >= sq.qn || rows <= a.few_rows) return;
+        kvh = head / a.share;
         row = tok * share + (int32_t)(head % a.share);
+        by = rows;
+        const int32_t row0 = row / MANY_ROWS * MANY_ROWS, row_end = row0 + MANY_ROWS < rows ? row0 + MANY_ROWS : rows;
+        used = split_of(keys_of(a, sq, prefix_of(a, s, sq), row0 / share, (row_end - 1) / share), a.many_splits).used;
+        if (used <= 1) return;
+        part = many_part(a, t, head) - row;                    // (one row only: the next is beyond `rows`)
+        stride = 1;
     }
-    if (row >= rows || (rows <= a.few_rows) != few) return;
-    const int32_t row0 = row / tile * tile, row_end = row0 + tile < rows ? row0 + tile : rows;
-    const KeyRange kr = keys_of(a, sq, prefix_of(a, s, sq), row0 / share, (row_end - 1) / share);
-    const int32_t used = few ? split_of(kr, a.few_splits, FEW_UNIT).used : split_of(kr, a.many_splits, MANY_UNIT).used;
-    if (used <= 1) return;                                     // the row is written already
-    const int64_t t = (int64_t)sq.q0 + row / share;
-    const int64_t part = few ? few_part(a, s, head / a.share, row) : many_part(a, t, head);
-    const float *ml = a.part_ml + part * 2;
-    float top = NONE;
-    for (int32_t i = threadIdx.x & 63; i < used; i += 64) top = max_f(top, ml[2 * i]);
-    for (int k = 1; k < 64; k *= 2) top = max_f(top, __shfl_xor(top, k));
-    const float base = top == NONE ? 0.f : top;
-    const uint32_t quads = a.head_dim / 4, groups = JOIN_THREADS / quads, group = threadIdx.x / quads, quad = threadIdx.x % quads;
-    f32x4 y{0, 0, 0, 0};
-    float all = 0.f;
-    if (group < groups)
-        for (int32_t i = (int32_t)group; i < used; i += (int32_t)groups) {
-            const float w = exp2_fast(ml[2 * i] - base);
-            all += ml[2 * i + 1] * w;
-            y += *(const f32x4 *)(a.part + (part + i) * a.head_dim + 4 * quad) * w;
+    for (; row < rows; row += by) {
+        const int64_t mine = part + row;
+        const float *ml = a.part_ml + 2 * mine;
+        float top = NONE;
+        for (int32_t i = threadIdx.x & 63; i < used; i += 64) top = max_f(top, ml[2 * stride * i]);
+        for (int k = 1; k < 64; k *= 2) top = max_f(top, __shfl_xor(top, k));
+        const float base = top == NONE ? 0.f : top;
+        const uint32_t quads = a.head_dim / 4, groups = JOIN_THREADS / quads, group = threadIdx.x / quads, quad = threadIdx.x % quads;
+        f32x4 y{0, 0, 0, 0};
+        float all = 0.f;
+        if (group < groups) {
+#pragma unroll 4
+            for (int32_t i = (int32_t)group; i < used; i += (int32_t)groups) {
+                const float w = exp2_fast(ml[2 * stride * i] - base);
+                all += ml[2 * stride * i + 1] * w;
+                y += *(const f32x4 *)(a.part + (mine + stride * i) * a.head_dim + 4 * quad) * w;
+            }
         }
-    sums[threadIdx.x] = y;
-    alls[threadIdx.x] = all;
-    __syncthreads();
-    if (threadIdx.x >= quads) return;
-    for (uint32_t k = 1; k < groups; k++) {
-        y += sums[k * quads + quad];
-        all += alls[k * quads + quad];
+        __syncthreads();
+        sums[threadIdx.x] = y;
+        alls[threadIdx.x] = all;
+        __syncthreads();
+        if (threadIdx.x < quads) {
+            for (uint32_t k = 1; k < groups; k++) {
+                y += sums[k * quads + quad];
+                all += alls[k * quads + quad];
+            }
+            const float inv = all == 0.f ? 0.f : 1.f / all;
+            bf16x4 z;
+            for (int i = 0; i < 4; i++) z[i] = (__bf16)(all == 0.f ? 0.f : y[i] * inv);
+            const int64_t t = (int64_t)sq.q0 + row / share, head = (int64_t)kvh * a.share + row % share;
+            *(bf16x4 *)(a.out + t * a.o_tok + head * a.o_head + 8 * quad) = z;
+        }
     }
-    const float inv = all == 0.f ? 0.f : 1.f / all;
-    bf16x4 z;
-    for (int i = 0; i < 4; i++) z[i] = (__bf16)(all == 0.f ? 0.f : y[i] * inv);
-    *(bf16x4 *)(a.out + t * a.o_tok + (int64_t)head * a.o_head + 8 * quad) = z;
 }
 
 // What a call launches: decided by shapes and the hints alone.
@@ -78,7 +92,7 @@ struct Shape {
     uint32_t kc;                   // 32-element pieces of a head in the kernels
     bool few, many;                // which kernels
     int32_t few_rows;
-    uint32_t few_tiles, few_splits, many_tiles, many_splits;
+    uint32_t few_tiles, few_goal, few_unit, few_items, few_joined, many_tiles, many_splits;
     uint64_t few_parts, many_parts;          // partial rows in the workspace
 };
 
@@ -101,12 +115,16 @@ Shape shape_of(const ecfa_cache *c, const ecfa_batch *b, uint32_t heads, uint32_
         p.few_tiles = share <= 16 ? 1 : 2;
         p.few_rows = p.few ? 16 * (int32_t)p.few_tiles : 0;
     }
-    p.few_splits = p.many_splits = 1;
-    if (p.few) {                   // enough workgroups for four on each compute unit, of 128 keys at least
-        const uint64_t whole = (uint64_t)b->n_seqs * c->kv_heads, want = (4ull * cus + whole - 1) / whole, most = (max_kv + 127) / 128;
-        const uint64_t n = want < most ? want : most;
-        p.few_splits = (uint32_t)(n < 1 ? 1 : n > 256 ? 256 : n);
-        if (p.few_splits > 1) p.few_parts = whole * 16 * p.few_tiles * p.few_splits;
+    p.many_splits = 1;
+    if (p.few) {                   // two workgroups on each compute unit, with a step for each wave at least; thousands of sequences need no pieces
+        const uint32_t bytes = p.kc * 32 * (c->dtype == ECFA_E4M3 ? 1 : 2);
+        p.few_unit = FEW_WAVES * (p.few_tiles > 1 ? 1 : bytes <= 64 ? 4 : bytes <= 128 ? 2 : 1);        // as in FewShape
+        const uint64_t want = (2ull * cus + c->kv_heads - 1) / c->kv_heads, pieces = (max_kv + 32 * p.few_unit - 1) / (32 * p.few_unit);
+        const uint64_t most = pieces * b->n_seqs;
+        p.few_goal = pieces <= 1 || b->n_seqs > 1024 ? 0 : (uint32_t)(want < most ? want : most);
+        p.few_items = p.few_goal + b->n_seqs;
+        p.few_joined = (uint32_t)(rows < 16 * p.few_tiles ? rows : 16 * p.few_tiles);
+        if (p.few_goal) p.few_parts = (uint64_t)p.few_items * c->kv_heads * 16 * p.few_tiles;
     }
     if (p.many) {                  // two on each compute unit, of 512 keys at least
         p.many_tiles = (uint32_t)((uint64_t)b->n_tokens * share / MANY_ROWS) + b->n_seqs;
@@ -120,6 +138,10 @@ Shape shape_of(const ecfa_cache *c, const ecfa_batch *b, uint32_t heads, uint32_
 
 uint64_t workspace_of(const Shape &p, uint32_t head_dim) { return (p.few_parts + p.many_parts) * (head_dim + 2) * 4; }
 
+uint64_t few_join_blocks(const ecfa_cache *c, const ecfa_batch *b, const Shape &p) { return p.few_goal ? (uint64_t)b->n_seqs * c->kv_heads * p.few_joined : 0; }
+
+uint64_t join_blocks(const ecfa_cache *c, const ecfa_batch *b, const Shape &p) { return few_join_blocks(c, b, p) + p.many_parts / p.many_splits; }
+
 int check_heads(const ecfa_cache *c, uint32_t heads)
 {
     return heads == 0 || heads > (1u << 20) || heads % c->kv_heads ? ECF8_E_ARG : ECF8_OK;
@@ -130,9 +152,9 @@ int check_counts(const ecfa_cache *c, const ecfa_batch *b, uint32_t heads, const
 {
     if ((uint64_t)b->n_tokens * (heads / c->kv_heads) > (1u << 30)) return ECF8_E_ARG;
     const uint64_t most = 0xffffff;
-    if (p.few && (uint64_t)b->n_seqs * c->kv_heads * p.few_splits > most) return ECF8_E_ARG;
+    if (p.few && (uint64_t)p.few_items * c->kv_heads > most) return ECF8_E_ARG;
     if (p.many && (uint64_t)p.many_tiles * c->kv_heads * p.many_splits > most) return ECF8_E_ARG;
-    return p.few_parts / p.few_splits + p.many_parts / p.many_splits > most ? ECF8_E_ARG : ECF8_OK;
+    return join_blocks(c, b, p) > most ? ECF8_E_ARG : ECF8_OK;
 }
 
 int check_attend_rows(const ecfa_rows *r, uint32_t n_tokens)
@@ -196,15 +218,22 @@ int ecfa_attend(const ecfa_cache *cache, const ecfa_batch *batch, const ecfa_att
     a.prefix = opts->d_prefix_len;
     a.scale_log2 = opts->scale * LOG2E;
     a.cap = opts->softcap;
+    a.cap_inv = opts->softcap > 0 ? 1.f / opts->softcap : 0.f;
     a.head_dim = cache->head_dim;
     a.heads = q->heads;
     a.kv_heads = cache->kv_heads;
     a.share = q->heads / cache->kv_heads;
+    a.by_share = divisor_of(a.share);
+    a.by_kv_heads = divisor_of(a.kv_heads);
+    a.by_items = divisor_of(p.few_items ? p.few_items : 1);
+    a.by_goal = divisor_of(p.few_goal ? p.few_goal : 1);
     a.causal = opts->causal;
     a.window = opts->window;
     a.few_rows = p.few_rows;
     a.few_tile = 16 * p.few_tiles;
-    a.few_splits = p.few_splits;
+    a.few_goal = p.few_goal;
+    a.few_unit = p.few_unit;
+    a.few_items = p.few_items;
     a.many_tiles = p.many_tiles;
     a.many_splits = p.many_splits;
     hipStream_t s = (hipStream_t)stream;
@@ -212,8 +241,8 @@ int ecfa_attend(const ecfa_cache *cache, const ecfa_batch *batch, const ecfa_att
     if (p.few) rc = f8 ? launch_few_rows_e4m3(a, p.kc, p.few_tiles, s) : launch_few_rows_bf16(a, p.kc, p.few_tiles, s);
     if (p.many && !rc) rc = f8 ? launch_many_rows_e4m3(a, p.kc, s) : launch_many_rows_bf16(a, p.kc, s);
     if (rc || !need) return rc;
-    const uint32_t few_blocks = (uint32_t)(p.few_parts / p.few_splits), blocks = few_blocks + (uint32_t)(p.many_parts / p.many_splits);
-    hipLaunchKernelGGL(ecfa_attend_join_kernel, dim3(blocks), dim3(JOIN_THREADS), 0, s, a, few_blocks);
+    hipLaunchKernelGGL(ecfa_attend_join_kernel, dim3((unsigned)join_blocks(cache, batch, p)), dim3(JOIN_THREADS), 0, s, a,
+                       (uint32_t)few_join_blocks(cache, batch, p), p.few_joined ? p.few_joined : 1u);
     return hipGetLastError() == hipSuccess ? ECF8_OK : ECF8_E_HIP;
 }
 

@@ -75,7 +75,7 @@ __global__ __launch_bounds__(MANY_WAVES * 64, KC <= 4 ? 2 : 1) void ecfa_attend_
     const int32_t share = (int32_t)a.share;
     const int32_t tok_a = row0 / share, tok_b = (row_end - 1) / share;
     const KeyRange kr = keys_of(a, sq, prefix, tok_a, tok_b);
-    const Split sp = split_of(kr, a.many_splits, MANY_UNIT);
+    const Split sp = split_of(kr, a.many_splits);
     const bool alone = sp.used <= 1;
     if ((int32_t)split >= (sp.used > 1 ? sp.used : 1)) return;
 
@@ -83,7 +83,7 @@ __global__ __launch_bounds__(MANY_WAVES * 64, KC <= 4 ? 2 : 1) void ecfa_attend_
     const int32_t *table = a.b.table + (int64_t)s * a.b.table_stride;
     const uint32_t in_page = (1u << a.c.page_shift) - 1;
     const float k_scale = a.c.k_scale ? a.c.k_scale[kvh] : 1.f, v_scale = a.c.v_scale ? a.c.v_scale[kvh] : 1.f;
-    const float to_log2 = a.scale_log2 * k_scale;
+    const float to_log2 = a.scale_log2 * k_scale, cap_in = to_log2 * 2.f * a.cap_inv;
 
     // this lane's row
     const int32_t r = row0 + 32 * wave + col;
@@ -110,11 +110,6 @@ __global__ __launch_bounds__(MANY_WAVES * 64, KC <= 4 ? 2 : 1) void ecfa_attend_
     float m = NONE, l = 0.f;
     int poison = 0;
 
-    if (a.head_dim < KC * 32 || KC == 3 || KC == 6) {          // what no load fills: zeros, for the products of elements past a head's end
-        for (int i = threadIdx.x * 16; i < 4 * S::TILE; i += MANY_WAVES * 64 * 16) *(u32x4 *)(lds + i) = u32x4{0, 0, 0, 0};
-        __syncthreads();
-    }
-
     const int32_t step_a = sp.first + (int32_t)split * sp.per;
     const int32_t step_b = step_a + sp.per < sp.first + sp.count ? step_a + sp.per : sp.first + sp.count;
 
@@ -136,38 +131,38 @@ __global__ __launch_bounds__(MANY_WAVES * 64, KC <= 4 ? 2 : 1) void ecfa_attend_
     constexpr int PER = 64 / LOAD_PIECES, LOADS = 16 / PER;    // rows of a load, loads
     const int load_row = lane / LOAD_PIECES, load_piece = lane % LOAD_PIECES;
     u32x4 kx[F8 ? LOADS : 1], vx[F8 ? LOADS : 1];
-    const auto fetch_rows = [&](int n, const uint8_t *ks, const uint8_t *vs, uint64_t ok, int buffer) {
-        const int row = 16 * wave + PER * n + load_row;
+    const auto fetch_rows = [&](int n, const uint8_t *ks, const uint8_t *vs, int buffer) {
         if constexpr (F8) {
-            const int off = 16 * load_piece < (int)a.head_dim ? 16 * load_piece : 0;
-            kx[n] = *(const u32x4 *)(ks + off);
-            vx[n] = *(const u32x4 *)(vs + off);
-            if (ok != ~0ull && !(ok >> row & 1)) vx[n] = u32x4{0, 0, 0, 0};
+            kx[n] = *(const u32x4 *)ks;
+            vx[n] = *(const u32x4 *)vs;
         } else {
-            const int off = 16 * (load_piece ^ spread<KC>(row & 15));
             uint8_t *dst = lds + buffer * 2 * S::TILE + (16 * wave + PER * n) * S::ROW;
-            if (off < 2 * (int)a.head_dim) {
-                __builtin_amdgcn_global_load_lds((hbm_u8 *)(ks + off), (lds_u8 *)dst, 16, 0, 0);
-                if (ok == ~0ull || (ok >> row & 1)) __builtin_amdgcn_global_load_lds((hbm_u8 *)(vs + off), (lds_u8 *)(dst + S::TILE), 16, 0, 0);
-                else *(u32x4 *)(dst + S::TILE + lane * 16) = u32x4{0, 0, 0, 0};
-            }
+            __builtin_amdgcn_global_load_lds((hbm_u8 *)ks, (lds_u8 *)dst, 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((hbm_u8 *)vs, (lds_u8 *)(dst + S::TILE), 16, 0, 0);
         }
     };
-    const int64_t k_lane = (int64_t)load_row * a.c.k_tok, v_lane = (int64_t)load_row * a.c.v_tok;
-    const auto fetch = [&](int32_t step, uint32_t e, uint64_t ok, int buffer) {
-        if (a.c.page_shift >= 4) {
+    const auto piece_of = [&](int n) {                         // bytes into a row; past the head's end its start again
+        const int off = 16 * (F8 ? load_piece : load_piece ^ spread<KC>(PER * n + load_row));
+        return off < (int)a.head_dim * (F8 ? 1 : 2) ? off : 0;
+    };
+    const bool near = a.c.page_shift >= 4 && a.c.near;         // sixteen keys lie in one page, and 32 bits reach over them
+    const auto fetch = [&](int32_t step, uint32_t e, int buffer) {
+        if (near) {
             const uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)e, 16 * wave);
-            const int64_t pg = first < a.c.n_pages ? first : 0u, in = (uint32_t)(32 * step + 16 * wave) & in_page;
-            const uint8_t *ks = k0 + pg * a.c.k_page + in * a.c.k_tok, *vs = v0 + pg * a.c.v_page + in * a.c.v_tok;
+            const uint64_t pg = first < a.c.n_pages ? first : 0u, in = (uint32_t)(32 * step + 16 * wave) & in_page;
+            const uint8_t *ks = k0 + pg * (uint64_t)a.c.k_page + in * (uint32_t)a.c.k_tok, *vs = v0 + pg * (uint64_t)a.c.v_page + in * (uint32_t)a.c.v_tok;
 #pragma unroll
-            for (int n = 0; n < LOADS; n++) fetch_rows(n, ks + n * PER * a.c.k_tok + k_lane, vs + n * PER * a.c.v_tok + v_lane, ok, buffer);
+            for (int n = 0; n < LOADS; n++) {
+                const uint32_t row = (uint32_t)(PER * n + load_row), piece = (uint32_t)piece_of(n);
+                fetch_rows(n, ks + (row * (uint32_t)a.c.k_tok + piece), vs + (row * (uint32_t)a.c.v_tok + piece), buffer);
+            }
         } else {
 #pragma unroll
             for (int n = 0; n < LOADS; n++) {
                 const int row = 16 * wave + PER * n + load_row;
                 const uint32_t mine = (uint32_t)__shfl((int)e, row);
                 const int64_t pg = mine < a.c.n_pages ? mine : 0u, in = (uint32_t)(32 * step + row) & in_page;
-                fetch_rows(n, k0 + pg * a.c.k_page + in * a.c.k_tok, v0 + pg * a.c.v_page + in * a.c.v_tok, ok, buffer);
+                fetch_rows(n, k0 + pg * a.c.k_page + in * a.c.k_tok + piece_of(n), v0 + pg * a.c.v_page + in * a.c.v_tok + piece_of(n), buffer);
             }
         }
     };
@@ -205,7 +200,7 @@ __global__ __launch_bounds__(MANY_WAVES * 64, KC <= 4 ? 2 : 1) void ecfa_attend_
 
     uint32_t entry = entry_of(step_a);
     uint64_t ok = seen_by_some(step_a, entry);
-    if (step_a < step_b) fetch(step_a, entry, ok, 0);
+    if (step_a < step_b) fetch(step_a, entry, 0);
     store(0);
     entry = entry_of(step_a + 2);
     int buffer = 0;
@@ -214,8 +209,15 @@ __global__ __launch_bounds__(MANY_WAVES * 64, KC <= 4 ? 2 : 1) void ecfa_attend_
         __syncthreads();                                       // this step's keys are here, and nobody reads the other buffer any more
         const uint64_t ok_now = ok;
         ok = seen_by_some(step + 2, entry);
-        if (step + 2 < step_b) fetch(step + 2, entry, ok, buffer ^ 1);
+        if (step + 2 < step_b) fetch(step + 2, entry, buffer ^ 1);
         entry = entry_of(step + 4);
+        if (ok_now != ~0ull) {                                 // values that nobody may see, as zeros (the same for all waves)
+            const int row = 16 * wave + lane / 4;
+            if (!(ok_now >> row & 1))
+#pragma unroll 1
+                for (int i = 16 * (lane % 4); i < S::ROW; i += 64) *(u32x4 *)(lds + (2 * buffer + 1) * S::TILE + row * S::ROW + i) = u32x4{0, 0, 0, 0};
+            __syncthreads();
+        }
         // Made anew each step, from three registers instead of kept in sixteen
         int ka = lds0 + buffer * 2 * S::TILE + k_at, va = lds0 + buffer * 2 * S::TILE + S::TILE + v_at, va8 = lds0 + buffer * 2 * S::TILE + S::TILE + v_at8;
         asm volatile("" : "+v"(ka), "+v"(va), "+v"(va8));
@@ -228,7 +230,8 @@ __global__ __launch_bounds__(MANY_WAVES * 64, KC <= 4 ? 2 : 1) void ecfa_attend_
         for (int c = 0; c < NC; c++)
 #pragma unroll
             for (int u = 0; u < 2; u++) {
-                const bf16x8 kf = *(lds_bf16x8 *)(uintptr_t)(uint32_t)((ka ^ c << 5) + u * 32 * S::ROW);
+                bf16x8 kf = *(lds_bf16x8 *)(uintptr_t)(uint32_t)((ka ^ c << 5) + u * 32 * S::ROW);
+                if (a.head_dim < KC * 32 && 16 * c >= (int)a.head_dim) kf = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});   // past the head's end
                 x[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[c], x[u], 0, 0, 0);
             }
         const int32_t key0 = 32 * step;
@@ -240,13 +243,12 @@ __global__ __launch_bounds__(MANY_WAVES * 64, KC <= 4 ? 2 : 1) void ecfa_attend_
 #pragma unroll
             for (int u = 0; u < 2; u++)
 #pragma unroll
-                for (int i = 0; i < 16; i++) {
-                    float y = x[u][i] * to_log2;
-                    if (a.cap > 0.f) y = capped(y, a.cap);
-                    const int32_t far = place - (key0 + 32 * u + 8 * (i / 4) + 4 * half + i % 4);
-                    y -= slope * (float)(far < 0 ? -far : far);
-                    x[u][i] = y;
-                }
+                for (int i = 0; i < 16; i++) x[u][i] = capped_or_scaled(a, x[u][i], to_log2, cap_in);
+            if (a.slopes)
+#pragma unroll
+                for (int u = 0; u < 2; u++)
+#pragma unroll
+                    for (int i = 0; i < 16; i++) x[u][i] = less_distance(x[u][i], slope, place - (key0 + 32 * u + 8 * (i / 4) + 4 * half + i % 4));
         }
         uint64_t seen = ~0ull;
         if (!whole) {
@@ -298,13 +300,15 @@ __global__ __launch_bounds__(MANY_WAVES * 64, KC <= 4 ? 2 : 1) void ecfa_attend_
 
         if (!whole && tok_b > tok_a) {                         // rows that see different keys: 0 * v is 0 unless v is NaN or infinite
             const bf16x8 zero = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
-            f32x16 z;
-            for (int i = 0; i < 16; i++) z[i] = 0.f;
-#pragma unroll
-            for (int d = 0; d < KC; d++)
+#pragma unroll 1
+            for (int d = 0; d < KC; d++) {
+                f32x16 z;
+                for (int i = 0; i < 16; i++) z[i] = 0.f;
 #pragma unroll
                 for (int n = 0; n < 4; n++) z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(va, va8, d, 16 * n), zero, z, 0, 0, 0);
-            for (int i = 0; i < 16; i++) poison |= z[i] != 0.f ? 1 : 0;
+                for (int i = 0; i < 16; i++)                   // (elements past the head's end are not its own)
+                    poison |= z[i] != 0.f && 32 * d + 8 * (i / 4) + 4 * half < (int)a.head_dim ? 1 : 0;
+            }
         }
 #pragma unroll
         for (int n = 0; n < 4; n++)
@@ -317,7 +321,7 @@ __global__ __launch_bounds__(MANY_WAVES * 64, KC <= 4 ? 2 : 1) void ecfa_attend_
     float all = sum_xor<32>(l);
     if (__any(poison)) {
         float y[16 * KC];
-        attend_slowly<F8, 2, 4 * KC>(a, a.q + t * a.q_tok + (int64_t)head * a.q_head, k0, v0, table, step_a, step_b, own, place, to_log2, slope, half,
+        attend_slowly<F8, 2, 4 * KC>(a, a.q + t * a.q_tok + (int64_t)head * a.q_head, k0, v0, table, step_a, step_b, 1, 1, own, place, to_log2, slope, half,
                                      [&](int n) { return 8 * n + 4 * half; }, y, m, all);
 #pragma unroll
         for (int d = 0; d < KC; d++)

@@ -22,6 +22,7 @@ struct CacheView {                           // strides in bytes
     const float *k_scale, *v_scale;
     int64_t k_page, k_tok, k_head, v_page, v_tok, v_head;
     uint32_t n_pages, page_shift;
+    uint32_t near;                           // tokens of a page lie less than 2^25 bytes apart: offsets over 16 of them fit 32 bits
 };
 
 struct BatchView {

@@ -29,6 +29,7 @@ inline int cache_view(const ecfa_cache *c, bool used, CacheView *o)
     o->v_tok = c->v_stride[1] * e;
     o->v_head = c->v_stride[2] * e;
     o->n_pages = c->n_pages;
+    o->near = o->k_tok >= 0 && o->v_tok >= 0 && o->k_tok < (1 << 25) && o->v_tok < (1 << 25);
     return ECF8_OK;
 }
 
