@@ -327,9 +327,7 @@ __device__ inline void attend_slowly(const AttendArgs &a, const uint8_t *q, cons
 }
 
 // Launches, one per cache type; kc = 32-element pieces of a head that the kernels are compiled for.
-int launch_few_rows_bf16(const AttendArgs &a, uint32_t kc, uint32_t tiles, hipStream_t s);
-int launch_few_rows_e4m3(const AttendArgs &a, uint32_t kc, uint32_t tiles, hipStream_t s);
-int launch_many_rows_bf16(const AttendArgs &a, uint32_t kc, hipStream_t s);
-int launch_many_rows_e4m3(const AttendArgs &a, uint32_t kc, hipStream_t s);
+int launch_attend_bf16(const AttendArgs &a, uint32_t kc, bool few, bool many, hipStream_t s);
+int launch_attend_e4m3(const AttendArgs &a, uint32_t kc, bool few, bool many, hipStream_t s);
 
 } // namespace ecfa

@@ -10,79 +10,84 @@ using namespace ecfa;
 
 constexpr int JOIN_THREADS = 256;
 
-// One workgroup for a (token, query head): the pieces' (m, l, O) to one row.  They are dealt to groups of head_dim / 4 threads, so
-// that all partial rows are on their way at once.  Reads what the pieces have written, 4 head_dim + 8 bytes each, once.
-// The first few_blocks workgroups are for the rows of the few-rows kernel's first tiles (few_joined of each sequence and key/value head
-// next to each other, and what lies beyond those in turn), the others for tokens of the other kernel.
+// The pieces' (m, l, O) of a row to one row: a thread four elements of it, from piece `first` on every `by`-th one.
+struct Joined {
+    f32x4 y;
+    float all;
+};
+__device__ inline Joined join(const AttendArgs &a, int64_t part, int64_t stride, int32_t used, int32_t first, int32_t by, float base, uint32_t quad)
+{
+    Joined j{f32x4{0, 0, 0, 0}, 0.f};
+#pragma unroll 4
+    for (int32_t i = first; i < used; i += by) {
+        const int64_t at = part + stride * i;
+        const float w = exp2_fast(a.part_ml[2 * at] - base);
+        j.all += a.part_ml[2 * at + 1] * w;
+        j.y += *(const f32x4 *)(a.part + at * a.head_dim + 4 * quad) * w;
+    }
+    return j;
+}
+
+__device__ inline void write_joined(const AttendArgs &a, const Joined &j, int64_t t, int64_t head, uint32_t quad)
+{
+    const float inv = j.all == 0.f ? 0.f : 1.f / j.all;
+    bf16x4 z;
+    for (int i = 0; i < 4; i++) z[i] = (__bf16)(j.all == 0.f ? 0.f : j.y[i] * inv);
+    *(bf16x4 *)(a.out + t * a.o_tok + head * a.o_head + 8 * quad) = z;
+}
+
+// Reads what the pieces have written, 4 head_dim + 8 bytes a row and piece, once.  The first few_blocks workgroups are for rows of the few-rows
+// kernel's first tiles, which may have hundreds of pieces: one workgroup a row (few_joined of each sequence and key/value head, and what lies
+// beyond those in turn), groups of head_dim / 4 threads share the pieces.  The others are for a token of the other kernel each, with few
+// pieces: head_dim / 4 threads a row.
 __global__ __launch_bounds__(JOIN_THREADS) void ecfa_attend_join_kernel(const AttendArgs a, uint32_t few_blocks, uint32_t few_joined)
 {
     __shared__ f32x4 sums[JOIN_THREADS];
     __shared__ float alls[JOIN_THREADS];
     const int32_t share = (int32_t)a.share;
-    int32_t row, used, rows, by;                               // row of the sequence and its key/value head
-    int64_t part, stride;                                      // its first partial row, and how far they lie apart
-    uint32_t kvh;
-    Seq sq;
-    if (blockIdx.x < few_blocks) {
-        row = (int32_t)(blockIdx.x % few_joined);
-        kvh = blockIdx.x / few_joined % a.kv_heads;
-        const uint32_t s = blockIdx.x / few_joined / a.kv_heads;
-        const FewItem it = few_plan(a, s, true);
-        if (!it.there || it.used <= 1) return;                 // not this kernel's, or written already
-        sq = seq_of(a.b, s);
-        rows = sq.qn * share;
-        rows = rows < (int32_t)a.few_tile ? rows : (int32_t)a.few_tile;
-        by = (int32_t)few_joined;
-        used = it.used;
-        part = few_part(a, it.first_item, kvh, 0);
-        stride = (int64_t)a.kv_heads * a.few_tile;
-    } else {
-        const uint32_t at = blockIdx.x - few_blocks, t = at / a.heads, head = at % a.heads, s = seq_of_row(a.b, t);
-        sq = seq_of(a.b, s);
-        const int32_t tok = (int32_t)t - sq.q0;
-        rows = sq.qn * share;
-        if (tok < 0 || tok >= sq.qn || rows <= a.few_rows) return;
-        kvh = head / a.share;
-        row = tok * share + (int32_t)(head % a.share);
-        by = rows;
-        const int32_t row0 = row / MANY_ROWS * MANY_ROWS, row_end = row0 + MANY_ROWS < rows ? row0 + MANY_ROWS : rows;
-        used = split_of(keys_of(a, sq, prefix_of(a, s, sq), row0 / share, (row_end - 1) / share), a.many_splits).used;
-        if (used <= 1) return;
-        part = many_part(a, t, head) - row;                    // (one row only: the next is beyond `rows`)
-        stride = 1;
+    const uint32_t quads = a.head_dim / 4, groups = JOIN_THREADS / quads, group = threadIdx.x / quads, quad = threadIdx.x % quads;
+    if (blockIdx.x >= few_blocks) {
+        const uint32_t t = blockIdx.x - few_blocks, s = seq_of_row(a.b, t);
+        const Seq sq = seq_of(a.b, s);
+        const int32_t tok = (int32_t)t - sq.q0, rows = sq.qn * share, prefix = prefix_of(a, s, sq);
+        if (tok < 0 || tok >= sq.qn || rows <= a.few_rows || group >= groups) return;
+        for (uint32_t head = group; head < a.heads; head += groups) {
+            const int32_t row = tok * share + (int32_t)(head - (uint32_t)over((int32_t)head, a.by_share) * a.share);
+            const int32_t row0 = row / MANY_ROWS * MANY_ROWS, row_end = row0 + MANY_ROWS < rows ? row0 + MANY_ROWS : rows;
+            const int32_t used = split_of(keys_of(a, sq, prefix, over(row0, a.by_share), over(row_end - 1, a.by_share)), a.many_splits).used;
+            if (used <= 1) continue;                           // written already
+            const int64_t part = many_part(a, t, head);
+            float top = NONE;
+            for (int32_t i = 0; i < used; i++) top = max_f(top, a.part_ml[2 * (part + i)]);
+            write_joined(a, join(a, part, 1, used, 0, 1, top == NONE ? 0.f : top, quad), t, head, quad);
+        }
+        return;
     }
-    for (; row < rows; row += by) {
-        const int64_t mine = part + row;
-        const float *ml = a.part_ml + 2 * mine;
+    const uint32_t kvh = blockIdx.x / few_joined % a.kv_heads, s = blockIdx.x / few_joined / a.kv_heads;
+    const FewItem it = few_plan(a, s, true);
+    if (!it.there || it.used <= 1) return;                     // not this kernel's, or written already
+    const Seq sq = seq_of(a.b, s);
+    const int32_t rows = sq.qn * share < (int32_t)a.few_tile ? sq.qn * share : (int32_t)a.few_tile;
+    const int64_t stride = (int64_t)a.kv_heads * a.few_tile;
+    for (int32_t row = (int32_t)(blockIdx.x % few_joined); row < rows; row += (int32_t)few_joined) {
+        const int64_t part = few_part(a, it.first_item, kvh, row);
         float top = NONE;
-        for (int32_t i = threadIdx.x & 63; i < used; i += 64) top = max_f(top, ml[2 * stride * i]);
+        for (int32_t i = threadIdx.x & 63; i < it.used; i += 64) top = max_f(top, a.part_ml[2 * (part + stride * i)]);
         for (int k = 1; k < 64; k *= 2) top = max_f(top, __shfl_xor(top, k));
         const float base = top == NONE ? 0.f : top;
-        const uint32_t quads = a.head_dim / 4, groups = JOIN_THREADS / quads, group = threadIdx.x / quads, quad = threadIdx.x % quads;
-        f32x4 y{0, 0, 0, 0};
-        float all = 0.f;
-        if (group < groups) {
-#pragma unroll 4
-            for (int32_t i = (int32_t)group; i < used; i += (int32_t)groups) {
-                const float w = exp2_fast(ml[2 * stride * i] - base);
-                all += ml[2 * stride * i + 1] * w;
-                y += *(const f32x4 *)(a.part + (mine + stride * i) * a.head_dim + 4 * quad) * w;
-            }
-        }
+        Joined j{f32x4{0, 0, 0, 0}, 0.f};
+        if (group < groups) j = join(a, part, stride, it.used, (int32_t)group, (int32_t)groups, base, quad);
         __syncthreads();
-        sums[threadIdx.x] = y;
-        alls[threadIdx.x] = all;
+        sums[threadIdx.x] = j.y;
+        alls[threadIdx.x] = j.all;
         __syncthreads();
         if (threadIdx.x < quads) {
             for (uint32_t k = 1; k < groups; k++) {
-                y += sums[k * quads + quad];
-                all += alls[k * quads + quad];
+                j.y += sums[k * quads + quad];
+                j.all += alls[k * quads + quad];
             }
-            const float inv = all == 0.f ? 0.f : 1.f / all;
-            bf16x4 z;
-            for (int i = 0; i < 4; i++) z[i] = (__bf16)(all == 0.f ? 0.f : y[i] * inv);
-            const int64_t t = (int64_t)sq.q0 + row / share, head = (int64_t)kvh * a.share + row % share;
-            *(bf16x4 *)(a.out + t * a.o_tok + head * a.o_head + 8 * quad) = z;
+            const int32_t tok = over(row, a.by_share);
+            write_joined(a, j, (int64_t)sq.q0 + tok, (int64_t)kvh * a.share + (row - tok * share), quad);
         }
     }
 }
@@ -128,7 +133,7 @@ Shape shape_of(const ecfa_cache *c, const ecfa_batch *b, uint32_t heads, uint32_
     }
     if (p.many) {                  // two on each compute unit, of 512 keys at least
         p.many_tiles = (uint32_t)((uint64_t)b->n_tokens * share / MANY_ROWS) + b->n_seqs;
-        const uint64_t whole = (uint64_t)p.many_tiles * c->kv_heads, want = 2ull * cus / whole, most = (max_kv + 511) / 512;
+        const uint64_t whole = (uint64_t)p.many_tiles * c->kv_heads, want = (2ull * cus + whole / 2) / whole, most = (max_kv + 511) / 512;
         const uint64_t n = want < most ? want : most;
         p.many_splits = (uint32_t)(n < 1 ? 1 : n);
         if (p.many_splits > 1) p.many_parts = (uint64_t)b->n_tokens * heads * p.many_splits;
@@ -140,7 +145,7 @@ uint64_t workspace_of(const Shape &p, uint32_t head_dim) { return (p.few_parts +
 
 uint64_t few_join_blocks(const ecfa_cache *c, const ecfa_batch *b, const Shape &p) { return p.few_goal ? (uint64_t)b->n_seqs * c->kv_heads * p.few_joined : 0; }
 
-uint64_t join_blocks(const ecfa_cache *c, const ecfa_batch *b, const Shape &p) { return few_join_blocks(c, b, p) + p.many_parts / p.many_splits; }
+uint64_t join_blocks(const ecfa_cache *c, const ecfa_batch *b, const Shape &p) { return few_join_blocks(c, b, p) + (p.many_parts ? b->n_tokens : 0u); }
 
 int check_heads(const ecfa_cache *c, uint32_t heads)
 {
@@ -152,8 +157,7 @@ int check_counts(const ecfa_cache *c, const ecfa_batch *b, uint32_t heads, const
 {
     if ((uint64_t)b->n_tokens * (heads / c->kv_heads) > (1u << 30)) return ECF8_E_ARG;
     const uint64_t most = 0xffffff;
-    if (p.few && (uint64_t)p.few_items * c->kv_heads > most) return ECF8_E_ARG;
-    if (p.many && (uint64_t)p.many_tiles * c->kv_heads * p.many_splits > most) return ECF8_E_ARG;
+    if ((uint64_t)(p.few ? p.few_items : 0) * c->kv_heads + (p.many ? (uint64_t)p.many_tiles * c->kv_heads * p.many_splits : 0) > most) return ECF8_E_ARG;
     return join_blocks(c, b, p) > most ? ECF8_E_ARG : ECF8_OK;
 }
 
@@ -238,8 +242,7 @@ int ecfa_attend(const ecfa_cache *cache, const ecfa_batch *batch, const ecfa_att
     a.many_splits = p.many_splits;
     hipStream_t s = (hipStream_t)stream;
     const bool f8 = cache->dtype == ECFA_E4M3;
-    if (p.few) rc = f8 ? launch_few_rows_e4m3(a, p.kc, p.few_tiles, s) : launch_few_rows_bf16(a, p.kc, p.few_tiles, s);
-    if (p.many && !rc) rc = f8 ? launch_many_rows_e4m3(a, p.kc, s) : launch_many_rows_bf16(a, p.kc, s);
+    rc = f8 ? launch_attend_e4m3(a, p.kc, p.few, p.many, s) : launch_attend_bf16(a, p.kc, p.few, p.many, s);
     if (rc || !need) return rc;
     hipLaunchKernelGGL(ecfa_attend_join_kernel, dim3((unsigned)join_blocks(cache, batch, p)), dim3(JOIN_THREADS), 0, s, a,
                        (uint32_t)few_join_blocks(cache, batch, p), p.few_joined ? p.few_joined : 1u);

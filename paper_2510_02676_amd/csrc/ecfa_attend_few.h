@@ -30,8 +30,9 @@ struct FewShape {
     }
 };
 
+// The work of workgroup `block`, with S::BYTES of LDS.
 template <int KC, bool F8, int NT>
-__global__ __launch_bounds__(FEW_WAVES * 64, KC <= 4 ? 2 : 1) void ecfa_attend_few_kernel(const AttendArgs a)
+__device__ __forceinline__ void attend_few(const AttendArgs &a, uint32_t block, uint8_t *lds)
 {
     using S = FewShape<KC, F8, NT>;
     typedef __attribute__((address_space(3))) uint8_t lds_u8;
@@ -40,10 +41,9 @@ __global__ __launch_bounds__(FEW_WAVES * 64, KC <= 4 ? 2 : 1) void ecfa_attend_f
     typedef __attribute__((ext_vector_type(2))) int i32x2;
     typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
     constexpr int E = S::E, KU = S::KU, ENTRIES = (KU + 1) / 2;
-    __shared__ __align__(16) uint8_t lds[S::BYTES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int g = lane / 16, col = lane % 16;
-    const uint32_t kvh = (uint32_t)over((int32_t)blockIdx.x, a.by_items), item = blockIdx.x - kvh * a.few_items;
+    const uint32_t kvh = (uint32_t)over((int32_t)block, a.by_items), item = block - kvh * a.few_items;
     const FewItem it = few_plan(a, item);
     if (!it.there) return;
     const uint32_t s = it.s;
@@ -413,25 +413,11 @@ __global__ __launch_bounds__(FEW_WAVES * 64, KC <= 4 ? 2 : 1) void ecfa_attend_f
     }
 }
 
-template <int KC, bool F8>
-int launch_few_rows_kc(const AttendArgs &a, uint32_t tiles, hipStream_t s)
+template <int KC, bool F8, int NT>
+__global__ __launch_bounds__(FEW_WAVES * 64, KC <= 4 ? 2 : 1) void ecfa_attend_few_kernel(const AttendArgs a)
 {
-    const uint64_t grid = (uint64_t)a.few_items * a.kv_heads;
-    if (tiles == 1) hipLaunchKernelGGL((ecfa_attend_few_kernel<KC, F8, 1>), dim3((unsigned)grid), dim3(FEW_WAVES * 64), 0, s, a);
-    else hipLaunchKernelGGL((ecfa_attend_few_kernel<KC, F8, 2>), dim3((unsigned)grid), dim3(FEW_WAVES * 64), 0, s, a);
-    return hipGetLastError() == hipSuccess ? ECF8_OK : ECF8_E_HIP;
-}
-
-template <bool F8>
-int launch_few_rows(const AttendArgs &a, uint32_t kc, uint32_t tiles, hipStream_t s)
-{
-    switch (kc) {
-    case 2: return launch_few_rows_kc<2, F8>(a, tiles, s);
-    case 3: return launch_few_rows_kc<3, F8>(a, tiles, s);
-    case 4: return launch_few_rows_kc<4, F8>(a, tiles, s);
-    case 6: return launch_few_rows_kc<6, F8>(a, tiles, s);
-    default: return launch_few_rows_kc<8, F8>(a, tiles, s);
-    }
+    __shared__ __align__(16) uint8_t lds[FewShape<KC, F8, NT>::BYTES];
+    attend_few<KC, F8, NT>(a, blockIdx.x, lds);
 }
 
 } // namespace ecfa

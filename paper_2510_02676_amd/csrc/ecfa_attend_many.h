@@ -48,20 +48,20 @@ __device__ inline uint32_t seq_of_tile(const AttendArgs &a, uint32_t tile)     /
     return lo;
 }
 
+// The work of workgroup `block`, with S::BYTES of LDS.
 template <int KC, bool F8, bool EXTRA>
-__global__ __launch_bounds__(MANY_WAVES * 64, KC <= 4 ? 2 : 1) void ecfa_attend_many_kernel(const AttendArgs a)
+__device__ __forceinline__ void attend_many(const AttendArgs &a, uint32_t block, uint8_t *lds)
 {
     using S = ManyShape<KC>;
     typedef __attribute__((address_space(3))) uint8_t lds_u8;
     typedef __attribute__((address_space(1))) const uint8_t hbm_u8;
     constexpr int NC = 2 * KC;                                 // pieces of 16 elements along a head
-    __shared__ __align__(16) uint8_t lds[S::BYTES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int half = lane / 32, col = lane % 32;
     // heads of keys next to each other in launch order: workgroups with the same keys then land on the same XCD where the heads
     // are a multiple of eight.  The last tiles, which see the most keys, go first.
-    const uint32_t kvh = blockIdx.x % a.kv_heads;
-    uint32_t at = blockIdx.x / a.kv_heads;
+    uint32_t at = (uint32_t)over((int32_t)block, a.by_kv_heads);
+    const uint32_t kvh = block - at * a.kv_heads;
     const uint32_t split = at % a.many_splits;
     at = a.many_tiles - 1 - at / a.many_splits;
     const uint32_t s = seq_of_tile(a, at);
@@ -73,7 +73,7 @@ __global__ __launch_bounds__(MANY_WAVES * 64, KC <= 4 ? 2 : 1) void ecfa_attend_
     const int32_t row_end = row0 + MANY_ROWS < rows ? row0 + MANY_ROWS : rows;
     const int32_t prefix = prefix_of(a, s, sq);
     const int32_t share = (int32_t)a.share;
-    const int32_t tok_a = row0 / share, tok_b = (row_end - 1) / share;
+    const int32_t tok_a = over(row0, a.by_share), tok_b = over(row_end - 1, a.by_share);
     const KeyRange kr = keys_of(a, sq, prefix, tok_a, tok_b);
     const Split sp = split_of(kr, a.many_splits);
     const bool alone = sp.used <= 1;
@@ -88,8 +88,8 @@ __global__ __launch_bounds__(MANY_WAVES * 64, KC <= 4 ? 2 : 1) void ecfa_attend_
     // this lane's row
     const int32_t r = row0 + 32 * wave + col;
     const bool there = r < row_end;
-    const int32_t tok = there ? r / share : tok_a;
-    const uint32_t head = kvh * a.share + (there ? (uint32_t)(r % share) : 0u);
+    const int32_t tok = there ? over(r, a.by_share) : tok_a;
+    const uint32_t head = kvh * a.share + (there ? (uint32_t)(r - tok * share) : 0u);
     const int64_t t = sq.q0 + tok;
     const int32_t place = sq.place0 + tok;
     const float slope = EXTRA && a.slopes ? a.slopes[head] * LOG2E : 0.f;
@@ -359,25 +359,11 @@ __global__ __launch_bounds__(MANY_WAVES * 64, KC <= 4 ? 2 : 1) void ecfa_attend_
     }
 }
 
-template <int KC, bool F8>
-int launch_many_rows_kc(const AttendArgs &a, hipStream_t s)
+template <int KC, bool F8, bool EXTRA>
+__global__ __launch_bounds__(MANY_WAVES * 64, KC <= 4 ? 2 : 1) void ecfa_attend_many_kernel(const AttendArgs a)
 {
-    const uint64_t grid = (uint64_t)a.many_tiles * a.kv_heads * a.many_splits;
-    if (a.cap > 0.f || a.slopes) hipLaunchKernelGGL((ecfa_attend_many_kernel<KC, F8, true>), dim3((unsigned)grid), dim3(MANY_WAVES * 64), 0, s, a);
-    else hipLaunchKernelGGL((ecfa_attend_many_kernel<KC, F8, false>), dim3((unsigned)grid), dim3(MANY_WAVES * 64), 0, s, a);
-    return hipGetLastError() == hipSuccess ? ECF8_OK : ECF8_E_HIP;
-}
-
-template <bool F8>
-int launch_many_rows(const AttendArgs &a, uint32_t kc, hipStream_t s)
-{
-    switch (kc) {
-    case 2: return launch_many_rows_kc<2, F8>(a, s);
-    case 3: return launch_many_rows_kc<3, F8>(a, s);
-    case 4: return launch_many_rows_kc<4, F8>(a, s);
-    case 6: return launch_many_rows_kc<6, F8>(a, s);
-    default: return launch_many_rows_kc<8, F8>(a, s);
-    }
+    __shared__ __align__(16) uint8_t lds[ManyShape<KC>::BYTES];
+    attend_many<KC, F8, EXTRA>(a, blockIdx.x, lds);
 }
 
 } // namespace ecfa
