@@ -11,6 +11,8 @@
 // they have to enter them again as P^T, eight keys a lane, so that P never goes through LDS.  V^T comes from row-major V
 // by the transposing LDS reads.
 #pragma once
+#include <type_traits>
+
 #include "ecfa_device.h"
 
 namespace ecfa {
@@ -257,6 +259,82 @@ __device__ inline void lds_fence_wave()
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// Transposing reads of V from LDS, several at a time, with the wait for them.  (As builtins each would first wait for all loads from memory
+// to LDS that are on their way, those of the next step too: the compiler does not know that they go to the other buffer.)
+// tr16: lane i of sixteen gives the place of four elements of row i / 4 and gets column i of the four rows; N fragments of eight keys from two
+// reads each, at at0[n] and at1[n], both `OFFSET` bytes on.  tr8: eight bytes of row i / 2, column i of eight rows, for each fragment one read.
+template <int OFFSET>
+__device__ __forceinline__ void tr16(const int (&at0)[2], const int (&at1)[2], bf16x8 *f)
+{
+    u32x2 a[2], b[2];
+    asm volatile("ds_read_b64_tr_b16 %0, %4 offset:%8\n\tds_read_b64_tr_b16 %1, %5 offset:%8\n\t"
+                 "ds_read_b64_tr_b16 %2, %6 offset:%8\n\tds_read_b64_tr_b16 %3, %7 offset:%8\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(a[0]), "=&v"(b[0]), "=&v"(a[1]), "=&v"(b[1])
+                 : "v"(at0[0]), "v"(at1[0]), "v"(at0[1]), "v"(at1[1]), "i"(OFFSET)
+                 : "memory");
+    for (int n = 0; n < 2; n++) f[n] = __builtin_bit_cast(bf16x8, u32x4{a[n][0], a[n][1], b[n][0], b[n][1]});
+}
+template <int OFFSET>
+__device__ __forceinline__ void tr16(const int (&at0)[3], const int (&at1)[3], bf16x8 *f)
+{
+    u32x2 a[3], b[3];
+    asm volatile("ds_read_b64_tr_b16 %0, %6 offset:%12\n\tds_read_b64_tr_b16 %1, %7 offset:%12\n\t"
+                 "ds_read_b64_tr_b16 %2, %8 offset:%12\n\tds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
+                 "ds_read_b64_tr_b16 %4, %10 offset:%12\n\tds_read_b64_tr_b16 %5, %11 offset:%12\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(a[0]), "=&v"(b[0]), "=&v"(a[1]), "=&v"(b[1]), "=&v"(a[2]), "=&v"(b[2])
+                 : "v"(at0[0]), "v"(at1[0]), "v"(at0[1]), "v"(at1[1]), "v"(at0[2]), "v"(at1[2]), "i"(OFFSET)
+                 : "memory");
+    for (int n = 0; n < 3; n++) f[n] = __builtin_bit_cast(bf16x8, u32x4{a[n][0], a[n][1], b[n][0], b[n][1]});
+}
+template <int OFFSET>
+__device__ __forceinline__ void tr16(const int (&at0)[4], const int (&at1)[4], bf16x8 *f)
+{
+    u32x2 a[4], b[4];
+    asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%16\n\tds_read_b64_tr_b16 %1, %9 offset:%16\n\t"
+                 "ds_read_b64_tr_b16 %2, %10 offset:%16\n\tds_read_b64_tr_b16 %3, %11 offset:%16\n\t"
+                 "ds_read_b64_tr_b16 %4, %12 offset:%16\n\tds_read_b64_tr_b16 %5, %13 offset:%16\n\t"
+                 "ds_read_b64_tr_b16 %6, %14 offset:%16\n\tds_read_b64_tr_b16 %7, %15 offset:%16\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(a[0]), "=&v"(b[0]), "=&v"(a[1]), "=&v"(b[1]), "=&v"(a[2]), "=&v"(b[2]), "=&v"(a[3]), "=&v"(b[3])
+                 : "v"(at0[0]), "v"(at1[0]), "v"(at0[1]), "v"(at1[1]), "v"(at0[2]), "v"(at1[2]), "v"(at0[3]), "v"(at1[3]), "i"(OFFSET)
+                 : "memory");
+    for (int n = 0; n < 4; n++) f[n] = __builtin_bit_cast(bf16x8, u32x4{a[n][0], a[n][1], b[n][0], b[n][1]});
+}
+template <int OFFSET>
+__device__ __forceinline__ void tr8(const int (&at)[2], u32x2 *f)
+{
+    asm volatile("ds_read_b64_tr_b8 %0, %2 offset:%4\n\tds_read_b64_tr_b8 %1, %3 offset:%4\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(f[0]), "=&v"(f[1])
+                 : "v"(at[0]), "v"(at[1]), "i"(OFFSET)
+                 : "memory");
+}
+template <int OFFSET>
+__device__ __forceinline__ void tr8(const int (&at)[3], u32x2 *f)
+{
+    asm volatile("ds_read_b64_tr_b8 %0, %3 offset:%6\n\tds_read_b64_tr_b8 %1, %4 offset:%6\n\tds_read_b64_tr_b8 %2, %5 offset:%6\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2])
+                 : "v"(at[0]), "v"(at[1]), "v"(at[2]), "i"(OFFSET)
+                 : "memory");
+}
+template <int OFFSET>
+__device__ __forceinline__ void tr8(const int (&at)[4], u32x2 *f)
+{
+    asm volatile("ds_read_b64_tr_b8 %0, %4 offset:%8\n\tds_read_b64_tr_b8 %1, %5 offset:%8\n\t"
+                 "ds_read_b64_tr_b8 %2, %6 offset:%8\n\tds_read_b64_tr_b8 %3, %7 offset:%8\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3])
+                 : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "i"(OFFSET)
+                 : "memory");
+}
+
+// f(integral_constant) for 0 .. N - 1: offsets in instructions are constants.
+template <int N, int I = 0, class F>
+__device__ __forceinline__ void times(F f)
+{
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>());
+        times<N, I + 1>(f);
+    }
 }
 
 // The slow way for one row: key by key, in fp32, from memory.  Taken where a value that some rows of a tile see and others do not

@@ -37,12 +37,8 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, uint32_t block, 
     using S = FewShape<KC, F8, NT>;
     typedef __attribute__((address_space(3))) uint8_t lds_u8;
     typedef __attribute__((address_space(1))) const uint8_t hbm_u8;
-    typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
-    typedef __attribute__((ext_vector_type(2))) int i32x2;
-    typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
     constexpr int E = S::E, KU = S::KU, ENTRIES = (KU + 1) / 2;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const int g = lane / 16, col = lane % 16;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const uint32_t kvh = (uint32_t)over((int32_t)block, a.by_items), item = block - kvh * a.few_items;
     const FewItem it = few_plan(a, item);
     if (!it.there) return;
@@ -62,6 +58,9 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, uint32_t block, 
     // max_q is a hint: if a sequence has more rows than a tile after all, the tiles follow one another
     for (int32_t row0 = 0; row0 < rows; row0 += 16 * NT) {
         if (row0 > 0 && it.split > 0) break;                   // later tiles are not split
+        int lane = threadIdx.x & 63;
+        asm volatile("" : "+v"(lane));                         // what follows from it is worked out here, and not kept for all tiles
+        const int g = lane / 16, col = lane % 16;
         const int32_t row_end = row0 + 16 * NT < rows ? row0 + 16 * NT : rows;
         const int32_t tok_a = over(row0, a.by_share), tok_b = over(row_end - 1, a.by_share);
         const KeyRange kr = keys_of(a, sq, prefix, tok_a, tok_b);
@@ -220,23 +219,25 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, uint32_t block, 
             // scores: x[n][u][i] belongs to row `col` and key 32 step + 16 u + 4 g + i
             f32x4 x[NT][2 * KU];
             if (begun) {
+                const auto scores = [&](auto ends) {           // `ends`: the head ends before the kernel's pieces do; zeros past its end
 #pragma unroll
-                for (int u = 0; u < 2 * KU; u++) {
+                    for (int u = 0; u < 2 * KU; u++) {
 #pragma unroll
-                    for (int n = 0; n < NT; n++) x[n][u] = f32x4{0, 0, 0, 0};
+                        for (int n = 0; n < NT; n++) x[n][u] = f32x4{0, 0, 0, 0};
 #pragma unroll
-                    for (int c = 0; c < KC; c++) {
-                        bf16x8 kf;
-                        if constexpr (F8) kf = bf16_of_e4m3(kx[u][c][0], kx[u][c][1]);
-                        else kf = __builtin_bit_cast(bf16x8, u32x4{kx[u][c][0], kx[u][c][1], kx[u][c][2], kx[u][c][3]});
-                        if (a.head_dim < KC * 32) {                // elements past the head's end: zero against zero
+                        for (int c = 0; c < KC; c++) {
+                            bf16x8 kf;
+                            if constexpr (F8) kf = bf16_of_e4m3(kx[u][c][0], kx[u][c][1]);
+                            else kf = __builtin_bit_cast(bf16x8, u32x4{kx[u][c][0], kx[u][c][1], kx[u][c][2], kx[u][c][3]});
                             const int d = F8 && c < (KC & ~1) ? 64 * (c / 2) + 16 * g + 8 * (c & 1) : 32 * c + 8 * g;
-                            if (d >= (int)a.head_dim) kf = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
-                        }
+                            if (ends.value && d >= (int)a.head_dim) kf = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
 #pragma unroll
-                        for (int n = 0; n < NT; n++) x[n][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[n][c], x[n][u], 0, 0, 0);
+                            for (int n = 0; n < NT; n++) x[n][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[n][c], x[n][u], 0, 0, 0);
+                        }
                     }
-                }
+                };
+                if (a.head_dim == KC * 32) scores(std::false_type());
+                else scores(std::true_type());
             }
             const int32_t key0 = 32 * step;
             const bool whole = all_ok && key0 >= kr.full_lo && key0 + S::KEYS <= kr.full_hi;
@@ -303,19 +304,26 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, uint32_t block, 
 
                 // O^T += V^T P^T, 32 keys at a time
                 const int vt = lds0 + buffer * S::V_BYTES;
-                const auto v_frag = [&](int k, int d) {
+                // Fragments d0 .. of the k-th 32 keys: sixteen elements of the head each
+                constexpr int D = KC == 3 || KC == 6 ? 3 : 4;
+                const auto v_frags = [&](auto k, int d0, bf16x8 *vf) {
+                    int at0[D], at1[D];
                     if constexpr (F8) {
                         const int row = (col / 2 < 4 ? 0 : 12) + 4 * g + col / 2;          // keys 4 g .. and 16 + 4 g ..
-                        const int src = vt + (32 * k + row) * S::ROW + 16 * (d ^ S::spread(row)) + 8 * (col & 1);
-                        const i32x2 y = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2 *)(uintptr_t)(uint32_t)src);
-                        return bf16_of_e4m3((uint32_t)y[0], (uint32_t)y[1]);
+#pragma unroll
+                        for (int d = 0; d < D; d++) at0[d] = vt + row * S::ROW + 16 * ((d0 + d) ^ S::spread(row)) + 8 * (col & 1);
+                        u32x2 y[D];
+                        tr8<k.value * 32 * S::ROW>(at0, y);
+#pragma unroll
+                        for (int d = 0; d < D; d++) vf[d] = bf16_of_e4m3(y[d][0], y[d][1]);
                     } else {
-                        const int row = 4 * g + col / 4, piece = 2 * d + col % 4 / 2;
-                        const int src = vt + (32 * k + row) * S::ROW + 16 * (piece ^ S::spread(row)) + 8 * (col & 1);
-                        const int src16 = vt + (32 * k + row + 16) * S::ROW + 16 * (piece ^ S::spread(row + 16)) + 8 * (col & 1);
-                        const bf16x4 y0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(uintptr_t)(uint32_t)src);
-                        const bf16x4 y1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(uintptr_t)(uint32_t)src16);
-                        return bf16x8{y0[0], y0[1], y0[2], y0[3], y1[0], y1[1], y1[2], y1[3]};
+                        const int row = 4 * g + col / 4, piece = 2 * d0 + col % 4 / 2;
+#pragma unroll
+                        for (int d = 0; d < D; d++) {
+                            at0[d] = vt + row * S::ROW + 16 * ((piece + 2 * d) ^ S::spread(row)) + 8 * (col & 1);
+                            at1[d] = vt + (row + 16) * S::ROW + 16 * ((piece + 2 * d) ^ S::spread(row + 16)) + 8 * (col & 1);
+                        }
+                        tr16<k.value * 32 * S::ROW>(at0, at1, vf);
                     }
                 };
                 if (!whole) {
@@ -330,23 +338,33 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, uint32_t block, 
                     lds_fence_wave();
                     if (tok_b > tok_a) {                       // rows that see different keys: 0 * v is 0 unless v is NaN or infinite
                         const bf16x8 zero = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
+                        times<KU>([&](auto k) {
 #pragma unroll 1
-                        for (int n = 0; n < KU * 2 * KC; n++) {
-                            const f32x4 z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_frag(n / (2 * KC), n % (2 * KC)), zero, f32x4{0, 0, 0, 0}, 0, 0, 0);
-                            const int e = 16 * (n % (2 * KC)) + 4 * g;         // elements past the head's end are not its own
-                            for (int i = 0; i < 4; i++) poison |= z[i] != 0.f && e < (int)a.head_dim ? 1 : 0;
-                        }
+                            for (int d0 = 0; d0 < 2 * KC; d0 += D) {
+                                bf16x8 vf[D];
+                                v_frags(k, d0, vf);
+#pragma unroll
+                                for (int d = 0; d < D; d++) {
+                                    const f32x4 z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[d], zero, f32x4{0, 0, 0, 0}, 0, 0, 0);
+                                    const int e = 16 * (d0 + d) + 4 * g;                  // elements past the head's end are not its own
+                                    for (int i = 0; i < 4; i++) poison |= z[i] != 0.f && e < (int)a.head_dim ? 1 : 0;
+                                }
+                            }
+                        });
                     }
                 }
+                times<KU>([&](auto k) {
 #pragma unroll
-                for (int k = 0; k < KU; k++)
+                    for (int d0 = 0; d0 < 2 * KC; d0 += D) {
+                        bf16x8 vf[D];
+                        v_frags(k, d0, vf);
 #pragma unroll
-                    for (int d = 0; d < 2 * KC; d++) {
-                        const bf16x8 vf = v_frag(k, d);
+                        for (int d = 0; d < D; d++)
 #pragma unroll
-                        for (int n = 0; n < NT; n++)
-                            o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(bf16x8, p[n][k]), o[n][d], 0, 0, 0);
+                            for (int n = 0; n < NT; n++)
+                                o[n][d0 + d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[d], __builtin_bit_cast(bf16x8, p[n][k.value]), o[n][d0 + d], 0, 0, 0);
                     }
+                });
             }
             begun = true;
             buffer ^= 1;
@@ -378,7 +396,9 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, uint32_t block, 
             if (g == 0) mj[wave * 16 + col] = m[n], lj[wave * 16 + col] = sum;
             __syncthreads();
             // sixteen threads a row: threadIdx / 16 is the row, and a thread takes four elements of each 64
-            const int r = threadIdx.x / 16, e = threadIdx.x % 16;
+            int tid = threadIdx.x;
+            asm volatile("" : "+v"(tid));                          // (nor this before the end)
+            const int r = tid / 16, e = tid % 16;
             float top = NONE;
             for (int w = 0; w < FEW_WAVES; w++) top = max_f(top, mj[w * 16 + r]);
             const float base = top == NONE ? 0.f : top;

@@ -188,14 +188,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, uint32_t block,
     const int vr = 4 * half + lane % 16 / 4, vp = 2 * (lane / 16 % 2) + lane % 4 / 2;
     const int v_at = vr * S::ROW + ((vp ^ spread<KC>(vr)) << 4) + 8 * (lane & 1);
     const int v_at8 = (vr + 8) * S::ROW + ((vp ^ spread<KC>(vr + 8)) << 4) + 8 * (lane & 1);
-    typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
     typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
-    // Eight keys of V: of 16 that begin at `keys`, elements 32 d .. of the head; `y0`, `y1`: this lane's places in the first 16 keys
-    const auto v_frag = [&](int y0, int y1, int d, int keys) {
-        const bf16x4 a0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(uintptr_t)(uint32_t)((y0 ^ d << 6) + keys * S::ROW));
-        const bf16x4 a1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(uintptr_t)(uint32_t)((y1 ^ d << 6) + keys * S::ROW));
-        return bf16x8{a0[0], a0[1], a0[2], a0[3], a1[0], a1[1], a1[2], a1[3]};
-    };
     const int lds0 = (int)(uint32_t)(uintptr_t)(lds_u8 *)lds;
 
     uint32_t entry = entry_of(step_a);
@@ -226,14 +219,18 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, uint32_t block,
         for (int u = 0; u < 2; u++)
 #pragma unroll
             for (int i = 0; i < 16; i++) x[u][i] = 0.f;
+        const auto scores = [&](auto ends) {                   // `ends`: the head ends before the kernel's pieces do; zeros past its end
 #pragma unroll
-        for (int c = 0; c < NC; c++)
+            for (int c = 0; c < NC; c++)
 #pragma unroll
-            for (int u = 0; u < 2; u++) {
-                bf16x8 kf = *(lds_bf16x8 *)(uintptr_t)(uint32_t)((ka ^ c << 5) + u * 32 * S::ROW);
-                if (a.head_dim < KC * 32 && 16 * c >= (int)a.head_dim) kf = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});   // past the head's end
-                x[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[c], x[u], 0, 0, 0);
-            }
+                for (int u = 0; u < 2; u++) {
+                    bf16x8 kf = *(lds_bf16x8 *)(uintptr_t)(uint32_t)((ka ^ c << 5) + u * 32 * S::ROW);
+                    if (ends.value && 16 * c >= (int)a.head_dim) kf = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
+                    x[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[c], x[u], 0, 0, 0);
+                }
+        };
+        if (a.head_dim == KC * 32) scores(std::false_type());
+        else scores(std::true_type());
         const int32_t key0 = 32 * step;
         const bool whole = ok_now == ~0ull && key0 >= kr.full_lo && key0 + 64 <= kr.full_hi;
         // x[u][i]: row `col`, key 32 u + 8 (i / 4) + 4 half + i % 4
@@ -304,16 +301,31 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, uint32_t block,
             for (int d = 0; d < KC; d++) {
                 f32x16 z;
                 for (int i = 0; i < 16; i++) z[i] = 0.f;
-#pragma unroll
-                for (int n = 0; n < 4; n++) z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(va, va8, d, 16 * n), zero, z, 0, 0, 0);
+                const int at0[2] = {va ^ d << 6, (va ^ d << 6) + 16 * S::ROW}, at1[2] = {va8 ^ d << 6, (va8 ^ d << 6) + 16 * S::ROW};
+                times<2>([&](auto n) {
+                    bf16x8 vf[2];
+                    tr16<n.value * 32 * S::ROW>(at0, at1, vf);
+                    z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[0], zero, z, 0, 0, 0);
+                    z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[1], zero, z, 0, 0, 0);
+                });
                 for (int i = 0; i < 16; i++)                   // (elements past the head's end are not its own)
                     poison |= z[i] != 0.f && 32 * d + 8 * (i / 4) + 4 * half < (int)a.head_dim ? 1 : 0;
             }
         }
+        // O^T += V^T P^T, sixteen keys at a time; their reads wait while the sixteen before are multiplied
+        constexpr int D = KC == 6 ? 3 : KC == 8 ? 4 : KC;      // pieces of the head at a time
 #pragma unroll
-        for (int n = 0; n < 4; n++)
+        for (int d0 = 0; d0 < KC; d0 += D) {
+            int at0[D], at1[D];
 #pragma unroll
-            for (int d = 0; d < KC; d++) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(va, va8, d, 16 * n), p[n], o[d], 0, 0, 0);
+            for (int d = 0; d < D; d++) at0[d] = va ^ (d0 + d) << 6, at1[d] = va8 ^ (d0 + d) << 6;
+            times<4>([&](auto n) {
+                bf16x8 vf[D];
+                tr16<n.value * 16 * S::ROW>(at0, at1, vf);
+#pragma unroll
+                for (int d = 0; d < D; d++) o[d0 + d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[d], p[n.value], o[d0 + d], 0, 0, 0);
+            });
+        }
         store(buffer ^ 1);
         buffer ^= 1;
     }
