@@ -266,17 +266,6 @@ __device__ inline void lds_fence_wave()
 // tr16: lane i of sixteen gives the place of four elements of row i / 4 and gets column i of the four rows; N fragments of eight keys from two
 // reads each, at at0[n] and at1[n], both `OFFSET` bytes on.  tr8: eight bytes of row i / 2, column i of eight rows, for each fragment one read.
 template <int OFFSET>
-__device__ __forceinline__ void tr16(const int (&at0)[2], const int (&at1)[2], bf16x8 *f)
-{
-    u32x2 a[2], b[2];
-    asm volatile("ds_read_b64_tr_b16 %0, %4 offset:%8\n\tds_read_b64_tr_b16 %1, %5 offset:%8\n\t"
-                 "ds_read_b64_tr_b16 %2, %6 offset:%8\n\tds_read_b64_tr_b16 %3, %7 offset:%8\n\ts_waitcnt lgkmcnt(0)"
-                 : "=&v"(a[0]), "=&v"(b[0]), "=&v"(a[1]), "=&v"(b[1])
-                 : "v"(at0[0]), "v"(at1[0]), "v"(at0[1]), "v"(at1[1]), "i"(OFFSET)
-                 : "memory");
-    for (int n = 0; n < 2; n++) f[n] = __builtin_bit_cast(bf16x8, u32x4{a[n][0], a[n][1], b[n][0], b[n][1]});
-}
-template <int OFFSET>
 __device__ __forceinline__ void tr16(const int (&at0)[3], const int (&at1)[3], bf16x8 *f)
 {
     u32x2 a[3], b[3];
@@ -300,14 +289,6 @@ __device__ __forceinline__ void tr16(const int (&at0)[4], const int (&at1)[4], b
                  : "v"(at0[0]), "v"(at1[0]), "v"(at0[1]), "v"(at1[1]), "v"(at0[2]), "v"(at1[2]), "v"(at0[3]), "v"(at1[3]), "i"(OFFSET)
                  : "memory");
     for (int n = 0; n < 4; n++) f[n] = __builtin_bit_cast(bf16x8, u32x4{a[n][0], a[n][1], b[n][0], b[n][1]});
-}
-template <int OFFSET>
-__device__ __forceinline__ void tr8(const int (&at)[2], u32x2 *f)
-{
-    asm volatile("ds_read_b64_tr_b8 %0, %2 offset:%4\n\tds_read_b64_tr_b8 %1, %3 offset:%4\n\ts_waitcnt lgkmcnt(0)"
-                 : "=&v"(f[0]), "=&v"(f[1])
-                 : "v"(at[0]), "v"(at[1]), "i"(OFFSET)
-                 : "memory");
 }
 template <int OFFSET>
 __device__ __forceinline__ void tr8(const int (&at)[3], u32x2 *f)

@@ -189,6 +189,13 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, uint32_t block,
     const int v_at = vr * S::ROW + ((vp ^ spread<KC>(vr)) << 4) + 8 * (lane & 1);
     const int v_at8 = (vr + 8) * S::ROW + ((vp ^ spread<KC>(vr + 8)) << 4) + 8 * (lane & 1);
     typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
+    typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
+    // Eight keys of V: of 16 that begin at `keys`, elements 32 d .. of the head; `y0`, `y1`: this lane's places in the first 16 keys
+    const auto v_frag = [&](int y0, int y1, int d, int keys) {
+        const bf16x4 a0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(uintptr_t)(uint32_t)((y0 ^ d << 6) + keys * S::ROW));
+        const bf16x4 a1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(uintptr_t)(uint32_t)((y1 ^ d << 6) + keys * S::ROW));
+        return bf16x8{a0[0], a0[1], a0[2], a0[3], a1[0], a1[1], a1[2], a1[3]};
+    };
     const int lds0 = (int)(uint32_t)(uintptr_t)(lds_u8 *)lds;
 
     uint32_t entry = entry_of(step_a);
@@ -228,6 +235,15 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, uint32_t block,
                     if (ends.value && 16 * c >= (int)a.head_dim) kf = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
                     x[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[c], x[u], 0, 0, 0);
                 }
+            if constexpr (!ends.value) {                       // reads four ahead of the products (1 %)
+                __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+                for (int i = 0; i < 2 * NC - 4; i++) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                }
+                __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+            }
         };
         if (a.head_dim == KC * 32) scores(std::false_type());
         else scores(std::true_type());
@@ -301,31 +317,18 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, uint32_t block,
             for (int d = 0; d < KC; d++) {
                 f32x16 z;
                 for (int i = 0; i < 16; i++) z[i] = 0.f;
-                const int at0[2] = {va ^ d << 6, (va ^ d << 6) + 16 * S::ROW}, at1[2] = {va8 ^ d << 6, (va8 ^ d << 6) + 16 * S::ROW};
-                times<2>([&](auto n) {
-                    bf16x8 vf[2];
-                    tr16<n.value * 32 * S::ROW>(at0, at1, vf);
-                    z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[0], zero, z, 0, 0, 0);
-                    z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[1], zero, z, 0, 0, 0);
-                });
+#pragma unroll
+                for (int n = 0; n < 4; n++) z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(va, va8, d, 16 * n), zero, z, 0, 0, 0);
                 for (int i = 0; i < 16; i++)                   // (elements past the head's end are not its own)
                     poison |= z[i] != 0.f && 32 * d + 8 * (i / 4) + 4 * half < (int)a.head_dim ? 1 : 0;
             }
         }
-        // O^T += V^T P^T, sixteen keys at a time; their reads wait while the sixteen before are multiplied
-        constexpr int D = KC == 6 ? 3 : KC == 8 ? 4 : KC;      // pieces of the head at a time
+        // O^T += V^T P^T.  (The first read also waits for the next step's keys, which have been on their way since the barrier by then: reads
+        // that do not, as in the few-rows kernel, were 2 % slower here.)
 #pragma unroll
-        for (int d0 = 0; d0 < KC; d0 += D) {
-            int at0[D], at1[D];
+        for (int n = 0; n < 4; n++)
 #pragma unroll
-            for (int d = 0; d < D; d++) at0[d] = va ^ (d0 + d) << 6, at1[d] = va8 ^ (d0 + d) << 6;
-            times<4>([&](auto n) {
-                bf16x8 vf[D];
-                tr16<n.value * 16 * S::ROW>(at0, at1, vf);
-#pragma unroll
-                for (int d = 0; d < D; d++) o[d0 + d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[d], p[n.value], o[d0 + d], 0, 0, 0);
-            });
-        }
+            for (int d = 0; d < KC; d++) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(va, va8, d, 16 * n), p[n], o[d], 0, 0, 0);
         store(buffer ^ 1);
         buffer ^= 1;
     }

@@ -46,7 +46,10 @@ _lib.ecfa_attend_workspace_bytes.restype = _u64
 _lib.ecfa_attend.argtypes = [_P(_Cache), _P(_Batch), _P(_AttendOpts), _P(_Rows), _P(_Rows), _vp, _u64, _vp]
 _lib.ecfa_quant.argtypes = [_vp, _u32, _u64, _u64, _i64, _u32, _vp, _vp, _vp]
 
+_append, _attend, _quant = _lib.ecfa_append, _lib.ecfa_attend, _lib.ecfa_quant
+
 _DTYPE = {torch.float32: F32, torch.bfloat16: BF16}
+_BYTES = (torch.float8_e4m3fn, torch.uint8)
 
 
 def _bad(fn):
@@ -55,16 +58,14 @@ def _bad(fn):
 
 def _rows(fn, x, n_tokens, heads, dim):
     """A (tokens, heads, dim) tensor as the C structure: any strides, elements of a head next to each other."""
-    if x.dim() != 3 or x.shape[0] != n_tokens or x.shape[2] != dim or (heads and x.shape[1] != heads) or x.dtype not in _DTYPE:
+    shape, stride, dtype = x.shape, x.stride(), _DTYPE.get(x.dtype)
+    if len(shape) != 3 or shape[0] != n_tokens or shape[2] != dim or (heads and shape[1] != heads) or dtype is None or stride[2] != 1:
         raise _bad(fn)
-    s = x.stride()
-    if s[2] != 1:
-        raise _bad(fn)
-    return _Rows(x.data_ptr(), s[0], s[1], x.shape[1], _DTYPE[x.dtype])
+    return _Rows(x.data_ptr(), stride[0], stride[1], shape[1], dtype)
 
 
 def _i32(fn, t, shape):
-    if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous():
+    if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous():
         raise _bad(fn)
     return t.data_ptr()
 
@@ -72,7 +73,7 @@ def _i32(fn, t, shape):
 def _scale_ptr(t, heads):
     if t is None:
         return None
-    if t.dtype != torch.float32 or tuple(t.shape) != (heads,) or not t.is_contiguous():
+    if t.dtype != torch.float32 or t.shape != (heads,) or not t.is_contiguous():
         raise _bad("Cache")
     return t.data_ptr()
 
@@ -86,7 +87,7 @@ class Cache:
             raise _bad("Cache")
         if k.dtype == torch.bfloat16:
             dtype = BF16
-        elif k.dtype in (torch.float8_e4m3fn, torch.uint8):
+        elif k.dtype in _BYTES:
             dtype = E4M3
         else:
             raise _bad("Cache")
@@ -131,7 +132,7 @@ class Rope:
         if freq.dim() != 1 or freq.dtype != torch.int64 or not freq.is_contiguous():
             raise _bad("Rope")
         self.freq, self.pos = freq, pos
-        self.c = _Rope(freq.data_ptr(), None if pos is None else _i32("Rope", pos, tuple(pos.shape)), 2 * freq.numel(), int(interleaved), scale, 0)
+        self.c = _Rope(freq.data_ptr(), None if pos is None else _i32("Rope", pos, pos.shape), 2 * freq.numel(), int(interleaved), scale, 0)
 
 
 def ecfa_append(cache, batch, k=None, v=None, q=None, q_out=None, rope=None, stream=None):
@@ -150,8 +151,9 @@ def ecfa_append(cache, batch, k=None, v=None, q=None, q_out=None, rope=None, str
         ro = _rows("ecfa_append", q_out, n, q.shape[1], dim)
     elif q_out is not None:
         raise _bad("ecfa_append")
-    rc = _lib.ecfa_append(cache.c, batch.c, None if rope is None else rope.c, rq, rk, rv, ro, _e._stream_ptr(stream))
-    _e._check("ecfa_append", rc)
+    rc = _append(cache.c, batch.c, None if rope is None else rope.c, rq, rk, rv, ro, _e._stream_ptr(stream))
+    if rc:
+        _e._check("ecfa_append", rc)
     return q_out
 
 
@@ -171,34 +173,40 @@ def ecfa_attend(cache, batch, q, scale=None, causal=True, window=0, softcap=0.0,
     if out is None:
         out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
     ro = _rows("ecfa_attend", out, n, heads, dim)
-    if slopes is not None and (slopes.dtype != torch.float32 or tuple(slopes.shape) != (heads,) or not slopes.is_contiguous()):
+    if slopes is not None and (slopes.dtype != torch.float32 or slopes.shape != (heads,) or not slopes.is_contiguous()):
         raise _bad("ecfa_attend")
     if workspace is None:
         workspace = attend_workspace(cache, batch, heads)
         if workspace is not None and stream is not None:
             workspace.record_stream(stream)
     opts = _AttendOpts(dim ** -0.5 if scale is None else scale, softcap, None if slopes is None else slopes.data_ptr(),
-                       None if prefix is None else _i32("ecfa_attend", prefix, tuple(batch.kv_len.shape)), int(causal), window)
-    rc = _lib.ecfa_attend(cache.c, batch.c, opts, rq, ro, None if workspace is None else workspace.data_ptr(),
-                          0 if workspace is None else workspace.numel(), _e._stream_ptr(stream))
-    _e._check("ecfa_attend", rc)
+                       None if prefix is None else _i32("ecfa_attend", prefix, batch.kv_len.shape), int(causal), window)
+    rc = _attend(cache.c, batch.c, opts, rq, ro, None if workspace is None else workspace.data_ptr(),
+                 0 if workspace is None else workspace.numel(), _e._stream_ptr(stream))
+    if rc:
+        _e._check("ecfa_attend", rc)
     return out
 
 
 def ecfa_quant(x, group=0, q=None, scale=None, stream=None):
     """x (rows, cols) fp32 or BF16, rows of any stride, to (E4M3 (rows, cols), fp32 scales (rows,) or with group = 128 (rows, cols / 128));
     the result is a ``torch.float8_e4m3fn`` tensor unless q is given (uint8 or float8_e4m3fn, dense)."""
-    if x.dim() != 2 or x.dtype not in _DTYPE or (x.shape[1] > 1 and x.stride(1) != 1) or group not in (0, 128):
+    shape, dtype = x.shape, _DTYPE.get(x.dtype)
+    if len(shape) != 2 or dtype is None or group not in (0, 128):
         raise _bad("ecfa_quant")
-    rows, cols = x.shape
+    rows, cols = shape
+    row_stride, one = x.stride()
+    if cols > 1 and one != 1:
+        raise _bad("ecfa_quant")
     want = (rows, cols // 128) if group else (rows,)
     if q is None:
         q = torch.empty((rows, cols), dtype=torch.float8_e4m3fn, device=x.device)
     if scale is None:
         scale = torch.empty(want, dtype=torch.float32, device=x.device)
-    if (q.dtype not in (torch.float8_e4m3fn, torch.uint8) or tuple(q.shape) != (rows, cols) or not q.is_contiguous()
-            or scale.dtype != torch.float32 or tuple(scale.shape) != want or not scale.is_contiguous()):
+    if (q.dtype not in _BYTES or q.shape != shape or not q.is_contiguous() or scale.dtype != torch.float32 or scale.shape != want
+            or not scale.is_contiguous()):
         raise _bad("ecfa_quant")
-    _e._check("ecfa_quant", _lib.ecfa_quant(x.data_ptr(), _DTYPE[x.dtype], rows, cols, x.stride(0), group, q.data_ptr(), scale.data_ptr(),
-                                            _e._stream_ptr(stream)))
+    rc = _quant(x.data_ptr(), dtype, rows, cols, row_stride, group, q.data_ptr(), scale.data_ptr(), _e._stream_ptr(stream))
+    if rc:
+        _e._check("ecfa_quant", rc)
     return q, scale
