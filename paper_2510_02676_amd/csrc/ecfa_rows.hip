@@ -24,7 +24,7 @@ struct AppendArgs {
     const uint64_t *freq;
     const int32_t *pos;
     float rope_scale;
-    uint32_t rot_units, half_units;          // rot_dim / 16, in whole and by halves of a head: units of 16 elements
+    uint32_t rot_units;                      // rot_dim / 16
     uint32_t units;                          // head_dim / 16
     uint32_t slots;                          // heads that a workgroup holds at once
     uint32_t q_heads, kv_heads;
@@ -43,11 +43,20 @@ __device__ inline void load8(const uint8_t *p, float *x)
     }
 }
 
+// PAST: written past the caches, for what nobody reads before it would have left them.
+template <bool PAST, class T>
+__device__ inline void put(uint8_t *p, T y)
+{
+    if constexpr (PAST) __builtin_nontemporal_store(y, (T *)p);
+    else *(T *)p = y;
+}
+
+template <bool PAST>
 __device__ inline void store8_bf16(uint8_t *p, const float *x)
 {
     bf16x8 y;
     for (int i = 0; i < 8; i++) y[i] = (__bf16)x[i];          // to nearest even
-    *(bf16x8 *)p = y;
+    put<PAST>(p, y);
 }
 
 // Eight fp32 as E4M3, to nearest even, limited to the largest number of the format; NaN stays NaN.
@@ -67,7 +76,10 @@ __device__ inline u32x2 pack8_e4m3(const float *x)
 // halves, 16 u .. interleaved) and walks over the heads of q, k and v, so that its eight sines and cosines are made once.  The angle
 // is position times frequency modulo 2^64 of a turn: the upper 32 bits go to the sine unit, which takes turns, and the
 // error stays below 2^-24 of a turn at any position.
-template <bool F32, bool F8, bool INTERLEAVED>
+// Bound by memory: 6472 tokens of BF16 rows with 32 + 2 x 8 heads of 128 elements, 80 MB in and 80 out, take 29.7 us (5.4 TB/s); a single
+// token 3.6 us, the time of a launch and of three loads that follow one another (length, page, row).  128 and 512 threads a token: 37.8 and
+// 41.4 us where 256 took 37.4.
+template <bool F32, bool F8, bool INTERLEAVED, bool PAST>
 __global__ __launch_bounds__(APPEND_THREADS) void ecfa_append_kernel(const AppendArgs a)
 {
     const uint32_t t = blockIdx.x;
@@ -80,7 +92,7 @@ __global__ __launch_bounds__(APPEND_THREADS) void ecfa_append_kernel(const Appen
     const int32_t place = sq.place0 + i;
     const bool turns = u < a.rot_units;
     uint32_t e0 = 16 * u, e1 = 16 * u + 8;                     // elements of the two halves of this thread's 16
-    if (!INTERLEAVED && turns) e0 = 8 * u, e1 = 8 * a.half_units + 8 * u;
+    if (!INTERLEAVED && turns) e0 = 8 * u, e1 = 8 * a.rot_units + 8 * u;
     float c[8], sn[8];
     if (turns) {
         const int64_t pos = a.pos ? a.pos[t] : place;
@@ -121,8 +133,8 @@ __global__ __launch_bounds__(APPEND_THREADS) void ecfa_append_kernel(const Appen
         }
         if (is_q) {
             uint8_t *dst = a.q_out.d + (int64_t)t * a.q_out.tok + (int64_t)hh * a.q_out.head;
-            store8_bf16(dst + e0 * 2, x);
-            store8_bf16(dst + e1 * 2, x + 8);
+            store8_bf16<PAST>(dst + e0 * 2, x);
+            store8_bf16<PAST>(dst + e1 * 2, x + 8);
             continue;
         }
         const uint32_t d0 = is_v ? 16 * u : e0, d1 = is_v ? 16 * u + 8 : e1;
@@ -134,11 +146,11 @@ __global__ __launch_bounds__(APPEND_THREADS) void ecfa_append_kernel(const Appen
             for (int j = 0; j < 16; j++) x[j] *= inv;
         }
         if constexpr (F8) {
-            *(u32x2 *)(dst + d0 * DST) = pack8_e4m3(x);
-            *(u32x2 *)(dst + d1 * DST) = pack8_e4m3(x + 8);
+            put<PAST>(dst + d0 * DST, pack8_e4m3(x));
+            put<PAST>(dst + d1 * DST, pack8_e4m3(x + 8));
         } else {
-            store8_bf16(dst + d0 * DST, x);
-            store8_bf16(dst + d1 * DST, x + 8);
+            store8_bf16<PAST>(dst + d0 * DST, x);
+            store8_bf16<PAST>(dst + d1 * DST, x + 8);
         }
     }
 }
@@ -187,7 +199,7 @@ __device__ inline void store_e4m3(uint8_t *q, const float *x, float inv)
 {
     float y[8];
     for (int i = 0; i < 8; i++) y[i] = x[i] * inv;
-    *(u32x2 *)q = pack8_e4m3(y);
+    put<true>(q, pack8_e4m3(y));                               // (past the caches: with what reads it next 11.7 -> 10.3 us at 2048 x 4096)
 }
 
 // A scale per row: THREADS threads a row (four rows to a workgroup of 256 if they are 64), the row held in registers between its
@@ -238,30 +250,22 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void ecfa_quant_rows
     }
 }
 
-constexpr uint32_t GROUP_PIECES = 2;         // of eight columns that a thread takes
-
-// A scale per 128 columns: sixteen lanes a group, eight columns a lane.
+// A scale per 128 columns: sixteen lanes a group, eight columns a lane, 2048 columns a workgroup.  Bound by memory: 4096 x 14336 fp32 take 49 us
+// (6.0 TB/s of 235 MB in, 60 out); with two and four times as many columns a workgroup 52 and 54 us, since fewer are in flight at the end.
 template <bool F32>
 __global__ __launch_bounds__(256) void ecfa_quant_groups_kernel(const QuantArgs a)
 {
     constexpr int SRC = F32 ? 4 : 2;
     const uint64_t row = blockIdx.x / a.per_row;
-    const uint32_t first = (uint32_t)(blockIdx.x % a.per_row) * (GROUP_PIECES * 256) + threadIdx.x, pieces = a.cols / 8;
-    const uint8_t *x = a.x + (int64_t)row * a.row_bytes;
-    float y[GROUP_PIECES][8];
-#pragma unroll
-    for (uint32_t k = 0; k < GROUP_PIECES; k++)
-        if (first + k * 256 < pieces) load8<F32>(x + (uint64_t)(first + k * 256) * 8 * SRC, y[k]);
-#pragma unroll
-    for (uint32_t k = 0; k < GROUP_PIECES; k++) {
-        const uint32_t p = first + k * 256;
-        if (p >= pieces) break;                                // the sixteen lanes of a group leave together: pieces is a multiple of 16
-        const uint32_t m = most_of_lanes<16>(most8(y[k]));
-        float scale;
-        const float inv = inverse_and_scale(m, &scale);
-        if ((threadIdx.x & 15) == 0) a.scale[row * (a.cols / 128) + p / 16] = scale;
-        store_e4m3(a.q + row * a.cols + (uint64_t)p * 8, y[k], inv);
-    }
+    const uint32_t p = (uint32_t)(blockIdx.x % a.per_row) * 256 + threadIdx.x;
+    if (p >= a.cols / 8) return;                               // the sixteen lanes of a group together: there is a multiple of 16 pieces
+    float y[8];
+    load8<F32>(a.x + (int64_t)row * a.row_bytes + (uint64_t)p * 8 * SRC, y);
+    const uint32_t m = most_of_lanes<16>(most8(y));
+    float scale;
+    const float inv = inverse_and_scale(m, &scale);
+    if ((threadIdx.x & 15) == 0) a.scale[row * (a.cols / 128) + p / 16] = scale;
+    store_e4m3(a.q + row * a.cols + (uint64_t)p * 8, y, inv);
 }
 
 // Strides and addresses of rows of `dim` elements, `heads` of them a token.
@@ -281,11 +285,23 @@ RowsView rows_view(const ecfa_rows *r)
     return RowsView{(uint8_t *)r->d, r->token_stride * e, r->head_stride * e};
 }
 
-template <bool F32, bool F8>
+template <bool F32, bool F8, bool PAST>
 void launch_append(const AppendArgs &a, bool interleaved, hipStream_t s)
 {
-    if (interleaved) hipLaunchKernelGGL((ecfa_append_kernel<F32, F8, true>), dim3(a.b.n_tokens), dim3(APPEND_THREADS), 0, s, a);
-    else hipLaunchKernelGGL((ecfa_append_kernel<F32, F8, false>), dim3(a.b.n_tokens), dim3(APPEND_THREADS), 0, s, a);
+    if (interleaved) hipLaunchKernelGGL((ecfa_append_kernel<F32, F8, true, PAST>), dim3(a.b.n_tokens), dim3(APPEND_THREADS), 0, s, a);
+    else hipLaunchKernelGGL((ecfa_append_kernel<F32, F8, false, PAST>), dim3(a.b.n_tokens), dim3(APPEND_THREADS), 0, s, a);
+}
+
+// What is written is read by the attention that follows.  Up to the size of the L2 caches of the eight parts of the card together it is found
+// there (25 MB of a 2048-token chunk: 329 us with its attention, 332 if written past them); more of it is not, and
+// only drives out what else is (80 MB: 29.7 us past them, 37.4 us through them).
+constexpr uint64_t ALL_L2 = 32u << 20;
+
+template <bool F32, bool F8>
+void launch_append_of_size(const AppendArgs &a, uint64_t bytes, bool interleaved, hipStream_t s)
+{
+    if (bytes > ALL_L2) launch_append<F32, F8, true>(a, interleaved, s);
+    else launch_append<F32, F8, false>(a, interleaved, s);
 }
 
 template <bool F32>
@@ -375,7 +391,6 @@ int ecfa_append(const ecfa_cache *cache, const ecfa_batch *batch, const ecfa_rop
         a.rot_units = rope->rot_dim / 16;
         interleaved = rope->interleaved != 0;
     }
-    a.half_units = a.rot_units;
     a.slots = APPEND_THREADS / a.units;
     a.q = rows_view(q);
     a.k = rows_view(k);
@@ -384,8 +399,9 @@ int ecfa_append(const ecfa_cache *cache, const ecfa_batch *batch, const ecfa_rop
     if (batch->n_tokens == 0) return ECF8_OK;
     const bool f32 = src->dtype == ECFA_F32, f8 = cache->dtype == ECFA_E4M3;
     hipStream_t s = (hipStream_t)stream;
-    if (f32) f8 ? launch_append<true, true>(a, interleaved, s) : launch_append<true, false>(a, interleaved, s);
-    else f8 ? launch_append<false, true>(a, interleaved, s) : launch_append<false, false>(a, interleaved, s);
+    const uint64_t bytes = (uint64_t)batch->n_tokens * cache->head_dim * (2 * a.q_heads + (f8 ? 2 : 4) * a.kv_heads);
+    if (f32) f8 ? launch_append_of_size<true, true>(a, bytes, interleaved, s) : launch_append_of_size<true, false>(a, bytes, interleaved, s);
+    else f8 ? launch_append_of_size<false, true>(a, bytes, interleaved, s) : launch_append_of_size<false, false>(a, bytes, interleaved, s);
     return hipGetLastError() == hipSuccess ? ECF8_OK : ECF8_E_HIP;
 }
 
@@ -403,7 +419,7 @@ int ecfa_quant(const void *d_x, uint32_t dtype, uint64_t rows, uint64_t cols, in
     a.row_bytes = row_stride * e;
     a.rows = rows;
     a.cols = (uint32_t)cols;
-    a.per_row = (uint32_t)((cols / 8 + GROUP_PIECES * 256 - 1) / (GROUP_PIECES * 256));
+    a.per_row = (uint32_t)((cols / 8 + 255) / 256);
     if (rows > 1ull << 40) return ECF8_E_ARG;
     const uint64_t most = 0x3fffff / a.per_row;                // rows of a launch: its threads are counted in 32 bits, 1024 a row at most
     for (uint64_t left = rows; left; left -= a.rows) {

@@ -116,6 +116,14 @@ def test_pages(page):
     check_append([130, 1, 65], [67, 1, 65], page=page)
 
 
+@pytest.mark.parametrize("src", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_more_than_the_caches_hold(src, cache, interleaved):
+    """Over 32 MB of results, which are written another way."""
+    check_append([280, 9, 3], [270, 2, 1], heads=128, kv_heads=128, dim=256, rot=224, src=src, cache=cache, interleaved=interleaved)
+
+
 def test_positions_far_out():
     pos = [0, 1, 4095, 131071, 10 ** 6, 10 ** 6 + 1, 2 ** 31 - 1, -1, -7, 12345678]
     for interleaved in (False, True):

@@ -368,3 +368,84 @@ def test_a_workspace_that_is_too_small_or_missing():
     assert e.value.code == ecf8.E_ALIGN
     torch.cuda.synchronize()
     assert (out == 5).all()
+
+
+@pytest.mark.parametrize("qn", [1, 4, 50])
+def test_caps_and_slopes_of_any_size(qn):
+    """Caps on both sides of where the limit's formula changes, scores far beyond them, slopes that leave a few keys."""
+    for cap in (0.01, 1.0, 63.9, 64.0, 64.1, 1e4, 1e30):
+        check(Setting([90, 30], [qn, 1], dim=64), softcap=cap)
+        check(Setting([90, 30], [qn, 1], dim=64), softcap=cap, scale=7.0)
+    slopes = torch.tensor([0.0, 1e-6, 0.5, 3.0, 40.0, 1e4, -0.01, 0.25], device=DEV)
+    check(Setting([90, 30], [qn, 1], dim=64), slopes=slopes)
+    check(Setting([90, 30], [qn, 1], dim=64), slopes=slopes, softcap=100.0, window=40)
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(20, 1), (40, 2), (4, 1), (66, 2)])
+def test_chunks_and_single_tokens_together(heads, kv_heads):
+    """Long and short sequences in one batch, cut into pieces and not; more than 32 heads to a key/value head have no short ones."""
+    for kv, qn in (([700, 1100, 7, 0, 64], [90, 1, 1, 1, 3]), ([60, 5, 2000, 1], [33, 2, 1, 1])):
+        check(Setting(kv, qn, heads=heads, kv_heads=kv_heads, dim=64, cache="e4m3" if heads == 4 else "bf16"))
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+def test_tokens_of_a_pool_far_apart(cache):
+    """Tokens 2^25 bytes apart, the pages between one another's tokens: offsets within a page pass what 32 bits hold."""
+    apart, heads, dim, page = 1 << (24 if cache == "bf16" else 25), 2, 64, 128
+    s = Setting([75, 200, 33], [1, 20, 1], heads=4, kv_heads=heads, dim=dim, page=page, cache=cache)
+    mem = torch.zeros(2 * (page - 1) * apart + 4 * s.pages * heads * dim, dtype=s.k.dtype, device=DEV)
+    at = (heads * dim, 2 * apart, dim, 1)
+    k, v = (torch.as_strided(mem, (s.pages, page, heads, dim), at, first) for first in (0, 2 * s.pages * heads * dim))
+    k.copy_(s.k)
+    v.copy_(s.v)
+    want, size = s.want()
+    b, q = s.batch(), s.q.to(DEV)
+    c = ecfa.Cache(k, v, *(None if x is None else x.to(DEV) for x in (s.k_scale, s.v_scale)))
+    got = ecfa.ecfa_attend(c, b, q).cpu().double().numpy()
+    assert (np.abs(got - want) <= ref.attend_bound(want, size)).all()
+    if cache == "bf16":                                          # and each token alone
+        single = ecfa.Batch(b.page_table, b.kv_len)
+        one = ecfa.ecfa_attend(c, single, q[[0, 20, 21]].contiguous()).cpu().double().numpy()
+        assert (np.abs(one - want[[0, 20, 21]]) <= ref.attend_bound(want, size)[[0, 20, 21]]).all()
+
+
+def test_more_sequences_than_are_cut_into_pieces():
+    for n in (1024, 1025):
+        kv = [(i * 37) % 150 for i in range(n - 1)] + [900]
+        check(Setting(kv, [1] * n, heads=2, kv_heads=1, dim=32, single=True, page=32))
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("qn", [1, 3, 40, 100])
+@pytest.mark.parametrize("what", [float("nan"), float("inf")])
+def test_pieces_of_which_some_hold_nothing(cache, qn, what):
+    """Long sequences cut in pieces: holes that take up a whole piece, windows that leave most of them out, NaN in places that are not seen."""
+    s = Setting([2600, 1300], [qn, 1], heads=4, kv_heads=1, dim=64, cache=cache, holes=[(0, j, -1) for j in range(30, 100)], seed=qn)
+    check(s)
+    check(s, window=300)
+    check(s, prefix=torch.tensor([2600, 5], dtype=torch.int32, device=DEV))
+    clean, windowed = s.run(), s.run(window=300)
+    poison(s, (0, 2600 - qn - 300), what)
+    assert np.array_equal(s.run(window=300), windowed)
+    poison(s, (0, 2599), what)                                   # seen by the last token alone
+    got, (want, size) = s.run(window=300), s.want(window=300)
+    assert np.isnan(got[qn - 1]).all() and np.array_equal(got[qn:], windowed[qn:])
+    assert (np.abs(got - want) <= ref.attend_bound(want, size))[:qn - 1].all()
+    assert np.array_equal(s.run()[qn:], clean[qn:])
+
+
+def test_counts_that_a_launch_cannot_hold():
+    one = torch.zeros((1, 1, 16), dtype=torch.bfloat16, device=DEV)
+    pool = torch.zeros((2, 1, 16, 1, 16), dtype=torch.bfloat16, device=DEV)
+    table, n = torch.zeros((1, 1), dtype=torch.int32, device=DEV), 1 << 21
+    long = ecfa.Batch(table, torch.ones(1, dtype=torch.int32, device=DEV), torch.zeros(2, dtype=torch.int32, device=DEV), n_tokens=n)
+    q = one.expand(n, 1024, 16)
+    with pytest.raises(ecf8.Ecf8Error) as e:                     # 2^31 rows to a key/value head
+        ecfa.ecfa_attend(ecfa.Cache(pool[0], pool[1]), long, q, out=q)
+    assert e.value.code == ecf8.E_ARG
+    heads = torch.zeros((2, 1, 16, 64, 16), dtype=torch.bfloat16, device=DEV)
+    many = ecfa.Batch(table.expand(n, 1), torch.ones(n, dtype=torch.int32, device=DEV))
+    q = one.expand(n, 64, 16)
+    with pytest.raises(ecf8.Ecf8Error) as e:                     # 2^27 workgroups
+        ecfa.ecfa_attend(ecfa.Cache(heads[0], heads[1]), many, q, out=q)
+    assert e.value.code == ecf8.E_ARG
