@@ -10,20 +10,37 @@ using namespace ecfa;
 
 constexpr int JOIN_THREADS = 256;
 
-// The pieces' (m, l, O) of a row to one row: a thread four elements of it, from piece `first` on every `by`-th one.
+// The pieces' (m, l, O) of a row to one row: a thread four elements of it, from piece `first` on every `by`-th one, four pieces' at once.
 struct Joined {
+    float top, all;
     f32x4 y;
-    float all;
 };
-__device__ inline Joined join(const AttendArgs &a, int64_t part, int64_t stride, int32_t used, int32_t first, int32_t by, float base, uint32_t quad)
+__device__ inline Joined join(const AttendArgs &a, int64_t part, int64_t stride, int32_t used, int32_t first, int32_t by, uint32_t quad)
 {
-    Joined j{f32x4{0, 0, 0, 0}, 0.f};
-#pragma unroll 4
-    for (int32_t i = first; i < used; i += by) {
-        const int64_t at = part + stride * i;
-        const float w = exp2_fast(a.part_ml[2 * at] - base);
-        j.all += a.part_ml[2 * at + 1] * w;
-        j.y += *(const f32x4 *)(a.part + at * a.head_dim + 4 * quad) * w;
+    Joined j{NONE, 0.f, f32x4{0, 0, 0, 0}};
+    for (int32_t i = first; i < used; i += 4 * by) {
+        float m[4], l[4], top = j.top;
+        f32x4 y[4];
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            const int64_t at = part + stride * (i + k * by < used ? i + k * by : i);
+            m[k] = a.part_ml[2 * at];
+            l[k] = a.part_ml[2 * at + 1];
+            y[k] = *(const f32x4 *)(a.part + at * a.head_dim + 4 * quad);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; k++) top = max_f(top, m[k]);    // (one twice does not matter here)
+        const float base = top == NONE ? 0.f : top, old = exp2_fast(j.top - base);
+        j.all *= old;
+        j.y *= old;
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            if (i + k * by >= used) break;
+            const float w = exp2_fast(m[k] - base);
+            j.all += l[k] * w;
+            j.y += y[k] * w;
+        }
+        j.top = top;
     }
     return j;
 }
@@ -43,7 +60,7 @@ __device__ inline void write_joined(const AttendArgs &a, const Joined &j, int64_
 __global__ __launch_bounds__(JOIN_THREADS) void ecfa_attend_join_kernel(const AttendArgs a, uint32_t few_blocks, uint32_t few_joined)
 {
     __shared__ f32x4 sums[JOIN_THREADS];
-    __shared__ float alls[JOIN_THREADS];
+    __shared__ float alls[JOIN_THREADS], tops[JOIN_THREADS];
     const int32_t share = (int32_t)a.share;
     const uint32_t quads = a.head_dim / 4, groups = JOIN_THREADS / quads, group = threadIdx.x / quads, quad = threadIdx.x % quads;
     if (blockIdx.x >= few_blocks) {
@@ -57,9 +74,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void ecfa_attend_join_kernel(const At
             const int32_t used = split_of(keys_of(a, sq, prefix, over(row0, a.by_share), over(row_end - 1, a.by_share)), a.many_splits).used;
             if (used <= 1) continue;                           // written already
             const int64_t part = many_part(a, t, head);
-            float top = NONE;
-            for (int32_t i = 0; i < used; i++) top = max_f(top, a.part_ml[2 * (part + i)]);
-            write_joined(a, join(a, part, 1, used, 0, 1, top == NONE ? 0.f : top, quad), t, head, quad);
+            write_joined(a, join(a, part, 1, used, 0, 1, quad), t, head, quad);
         }
         return;
     }
@@ -71,20 +86,22 @@ __global__ __launch_bounds__(JOIN_THREADS) void ecfa_attend_join_kernel(const At
     const int64_t stride = (int64_t)a.kv_heads * a.few_tile;
     for (int32_t row = (int32_t)(blockIdx.x % few_joined); row < rows; row += (int32_t)few_joined) {
         const int64_t part = few_part(a, it.first_item, kvh, row);
-        float top = NONE;
-        for (int32_t i = threadIdx.x & 63; i < it.used; i += 64) top = max_f(top, a.part_ml[2 * (part + stride * i)]);
-        for (int k = 1; k < 64; k *= 2) top = max_f(top, __shfl_xor(top, k));
-        const float base = top == NONE ? 0.f : top;
-        Joined j{f32x4{0, 0, 0, 0}, 0.f};
-        if (group < groups) j = join(a, part, stride, it.used, (int32_t)group, (int32_t)groups, base, quad);
+        Joined j{NONE, 0.f, f32x4{0, 0, 0, 0}};
+        if (group < groups) j = join(a, part, stride, it.used, (int32_t)group, (int32_t)groups, quad);
         __syncthreads();
         sums[threadIdx.x] = j.y;
         alls[threadIdx.x] = j.all;
+        tops[threadIdx.x] = j.top;
         __syncthreads();
         if (threadIdx.x < quads) {
-            for (uint32_t k = 1; k < groups; k++) {
-                j.y += sums[k * quads + quad];
-                j.all += alls[k * quads + quad];
+            float top = NONE;
+            for (uint32_t k = 0; k < groups; k++) top = max_f(top, tops[k * quads + quad]);
+            const float base = top == NONE ? 0.f : top;
+            j = Joined{top, 0.f, f32x4{0, 0, 0, 0}};
+            for (uint32_t k = 0; k < groups; k++) {
+                const float w = exp2_fast(tops[k * quads + quad] - base);
+                j.all += alls[k * quads + quad] * w;
+                j.y += sums[k * quads + quad] * w;
             }
             const int32_t tok = over(row, a.by_share);
             write_joined(a, j, (int64_t)sq.q0 + tok, (int64_t)kvh * a.share + (row - tok * share), quad);
