@@ -132,10 +132,14 @@ int ecfa_append(const ecfa_cache *cache, const ecfa_batch *batch, const ecfa_rop
  * and softmax in fp32; the weights are rounded to BF16 before they meet the values, and
  * their sum is taken of the rounded ones.
  *
- * Long sequences with few rows are split among workgroups that leave partial sums in
- * d_workspace (DEVICE, 16-byte aligned, of ecfa_attend_workspace_bytes(); NULL where that is
- * 0), and a second kernel joins them; the split depends on shapes and lengths alone, so the
- * same call gives the same bits.  Calls that overlap in time need a workspace each.
+ * Where there are few rows, long sequences are split among workgroups that leave partial sums in
+ * d_workspace (DEVICE, 16-byte aligned, of ecfa_attend_workspace_bytes(), which serves any options
+ * of a call with this batch; NULL where that is 0), and a second kernel joins them; the split
+ * depends on shapes, options and lengths alone, so the same call gives the same bits.  Calls that
+ * overlap in time need a workspace each.
+ * ECF8_E_ARG also: over 2^30 rows to a key/value head (n_tokens * q->heads / kv_heads) or over 2^24
+ * workgroups, which 2^20 single tokens with 8 key/value heads come near; ecfa_attend_workspace_bytes
+ * is 0 then.
  */
 typedef struct ecfa_attend_opts {
     float scale;                   /* > 0                                               */

@@ -109,7 +109,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void ecfa_attend_join_kernel(const At
     }
 }
 
-// What a call launches: decided by shapes and the hints alone.
+// What a call launches: decided by shapes, the hints and the window alone.
 struct Shape {
     uint32_t kc;                   // 32-element pieces of a head in the kernels
     bool few, many;                // which kernels
@@ -118,7 +118,32 @@ struct Shape {
     uint64_t few_parts, many_parts;          // partial rows in the workspace
 };
 
-Shape shape_of(const ecfa_cache *c, const ecfa_batch *b, uint32_t heads, uint32_t cus)
+// Pieces of the keys of each tile of many rows.  Where the tiles leave compute units free, in as many pieces, of 512 keys at least, as make the
+// last workgroup end first: rounds of two workgroups on each compute unit (one for heads of more than 128 elements, by registers), each
+// the steps of 64 keys of a piece and a start of about four steps' time; for the second kernel as much again, and a little for each piece.
+// (192 tiles of 8768 keys: 5 pieces 136 us, 3 pieces 160; 300 tiles of 9200: 3 pieces 204, 2 pieces 234.)  More tiles than
+// that are of unlike length and fill one another's gaps (512 tiles of 10240 keys: whole 255 us, in two 272).
+uint32_t splits_of(uint64_t tiles, uint64_t slots, uint64_t keys)
+{
+    if (tiles > slots || keys <= 512) return 1;
+    const double steps = (double)keys / 64, piece = 0.3;
+    double best = steps + 4;
+    uint64_t best_n = 1;
+    for (uint64_t rounds = 1; rounds <= 4; rounds++) {         // the most pieces that so many rounds hold, or the best number if it is less
+        uint64_t n = rounds * slots / tiles;
+        const uint64_t enough = (uint64_t)std::sqrt(steps * (double)rounds / piece), most = (keys + 511) / 512;
+        n = n < enough ? n : enough;
+        n = n < most ? n : most;
+        if (n < 2) continue;
+        const double t = (double)((n * tiles + slots - 1) / slots) * (steps / (double)n + 4) + 4 + piece * (double)n;
+        if (t < best) best = t, best_n = n;
+    }
+    return (uint32_t)best_n;
+}
+
+// Up to 32 rows of a sequence (the heads that share their keys, times its new tokens) go to the few-rows kernel, which reads K and V without
+// waiting for other waves; more go to 128-row tiles.  `window`: 0 if there is none; with one, no more is asked for than without.
+Shape shape_of(const ecfa_cache *c, const ecfa_batch *b, uint32_t heads, uint32_t cus, uint64_t window)
 {
     Shape p{};
     const uint32_t kc = (c->head_dim + 31) / 32, share = heads / c->kv_heads;
@@ -126,6 +151,7 @@ Shape shape_of(const ecfa_cache *c, const ecfa_batch *b, uint32_t heads, uint32_
     const uint32_t max_q = !b->d_q_start ? 1 : b->max_q && b->max_q < b->n_tokens ? b->max_q : b->n_tokens;
     const uint64_t keys = (uint64_t)b->table_width * c->page_size;
     const uint64_t max_kv = b->max_kv && b->max_kv < keys ? b->max_kv : keys;
+    const auto seen = [&](uint64_t rows) { return window && window + rows < max_kv ? window + rows : max_kv; };    // keys of a tile
     const uint64_t rows = (uint64_t)max_q * share;
     if (rows <= 32) {              // few rows everywhere
         p.few = true;
@@ -141,18 +167,19 @@ Shape shape_of(const ecfa_cache *c, const ecfa_batch *b, uint32_t heads, uint32_
     if (p.few) {                   // two workgroups on each compute unit, with a step for each wave at least; thousands of sequences need no pieces
         const uint32_t bytes = p.kc * 32 * (c->dtype == ECFA_E4M3 ? 1 : 2);
         p.few_unit = FEW_WAVES * (p.few_tiles > 1 ? 1 : bytes <= 64 ? 4 : bytes <= 128 ? 2 : 1);        // as in FewShape
-        const uint64_t want = (2ull * cus + c->kv_heads - 1) / c->kv_heads, pieces = (max_kv + 32 * p.few_unit - 1) / (32 * p.few_unit);
+        const uint64_t want = (2ull * cus + c->kv_heads - 1) / c->kv_heads, pieces = (seen(16 * p.few_tiles) + 32 * p.few_unit - 1) / (32 * p.few_unit);
         const uint64_t most = pieces * b->n_seqs;
         p.few_goal = pieces <= 1 || b->n_seqs > 1024 ? 0 : (uint32_t)(want < most ? want : most);
         p.few_items = p.few_goal + b->n_seqs;
         p.few_joined = (uint32_t)(rows < 16 * p.few_tiles ? rows : 16 * p.few_tiles);
         if (p.few_goal) p.few_parts = (uint64_t)p.few_items * c->kv_heads * 16 * p.few_tiles;
     }
-    if (p.many) {                  // two on each compute unit, of 512 keys at least
+    if (p.many) {
         p.many_tiles = (uint32_t)((uint64_t)b->n_tokens * share / MANY_ROWS) + b->n_seqs;
-        const uint64_t whole = (uint64_t)p.many_tiles * c->kv_heads, want = (2ull * cus + whole / 2) / whole, most = (max_kv + 511) / 512;
-        const uint64_t n = want < most ? want : most;
-        p.many_splits = (uint32_t)(n < 1 ? 1 : n);
+        const uint64_t slots = (kc <= 4 ? 2ull : 1ull) * cus, tiles = ((uint64_t)b->n_tokens * share + MANY_ROWS - 1) / MANY_ROWS * c->kv_heads;
+        p.many_splits = splits_of(tiles, slots, max_kv);
+        const uint32_t n = splits_of(tiles, slots, seen(MANY_ROWS));
+        if (n < p.many_splits) p.many_splits = n;              // with a window no more than without: the workspace is sized without
         if (p.many_splits > 1) p.many_parts = (uint64_t)b->n_tokens * heads * p.many_splits;
     }
     return p;
@@ -196,7 +223,7 @@ uint64_t ecfa_attend_workspace_bytes(const ecfa_cache *cache, const ecfa_batch *
     BatchView b{};
     if (!cache || !batch || cache_view(cache, true, &c) || batch_view(cache, batch, true, &b) || check_heads(cache, heads) || !batch->n_tokens) return 0;
     const int cus = device_cus();
-    const Shape p = shape_of(cache, batch, heads, cus > 0 ? (uint32_t)cus : 256u);
+    const Shape p = shape_of(cache, batch, heads, cus > 0 ? (uint32_t)cus : 256u, 0);
     return check_counts(cache, batch, heads, p) ? 0 : workspace_of(p, cache->head_dim);
 }
 
@@ -218,7 +245,7 @@ int ecfa_attend(const ecfa_cache *cache, const ecfa_batch *batch, const ecfa_att
     if (batch->n_tokens == 0) return ECF8_OK;
     const int cus = device_cus();
     if (cus <= 0) return ECF8_E_HIP;
-    const Shape p = shape_of(cache, batch, q->heads, (uint32_t)cus);
+    const Shape p = shape_of(cache, batch, q->heads, (uint32_t)cus, opts->causal ? opts->window : 0);
     if ((rc = check_counts(cache, batch, q->heads, p))) return rc;
     const uint64_t need = workspace_of(p, cache->head_dim);
     if (need) {
