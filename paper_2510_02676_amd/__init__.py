@@ -4,10 +4,11 @@
 (loaded on first use; importing it fails loudly when the library is not built);
 ``paper_2510_02676_amd.ecfw`` binds the wide-alphabet (E5M2, BF16) calls;
 ``paper_2510_02676_amd.ecfa`` binds the attention between a layer's compressed projections;
+``paper_2510_02676_amd.attention`` puts both together: the attention of a layer, its weights compressed;
 ``paper_2510_02676_amd.synth`` makes the seeded synthetic inputs.
 """
 
-__all__ = ["ecf8", "ecfw", "ecfa", "synth"]
+__all__ = ["ecf8", "ecfw", "ecfa", "attention", "synth"]
 
 
 def __getattr__(name):

@@ -1,0 +1,117 @@
+"""A layer's attention with compressed projections, step by step against 64 bits: every stage from what the stage before it left."""
+import numpy as np
+import pytest
+import torch
+
+import attention_reference as ref
+from paper_2510_02676_amd import ecf8, ecfa, synth
+from paper_2510_02676_amd.attention import CompressedAttention
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def weight(rows, cols, seed):
+    w = synth.make_weight(rows, cols, 1.7, 0.02, seed).numpy()
+    g = torch.Generator().manual_seed(seed)
+    scale = (torch.rand((-(-rows // 128), cols // 128), generator=g) * 0.5 + 0.5) * 2.0 ** -9
+    blob = ecf8.ecf8_encode(w, lane_syms=64, tile_rows=16)
+    wide = np.repeat(np.repeat(scale.double().numpy(), 128, 0)[:rows], 128, 1)
+    return (blob.header, blob.to(DEV), scale.to(DEV)), ref.E4M3[w] * wide
+
+
+def close_product(y, x8, x_scale, w):
+    """The FP8 matrix cores' own bound, 7 * 2^-13 of the sum of |x w|, and 32-bit scaling and sums."""
+    x = ref.E4M3[x8.cpu().numpy()] * np.repeat(x_scale.cpu().double().numpy(), 128, 1)
+    return (np.abs(y.cpu().double().numpy() - x @ w.T) <= (7 * 2.0 ** -13 + 2.0 ** -18) * (np.abs(x) @ np.abs(w).T) + 1e-30).all()
+
+
+def close_quant(x8, scale, x):
+    """Half a step: 2^-4 of a value, or half of the smallest number where that is more; and fp32 rounding of the quotient."""
+    x = x.cpu().double().numpy().reshape(x8.shape)
+    by = np.repeat(scale.cpu().double().numpy(), 128, 1)
+    return (np.abs(ref.E4M3[x8.cpu().numpy()] * by - x) <= (2.0 ** -4 + 2.0 ** -20) * np.abs(x) + 2.0 ** -10 * by).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("kv,qn", [([40, 700, 1], [1, 1, 1]), ([50, 33], [20, 3])])
+def test_a_step(kind, kv, qn):
+    heads, kv_heads, dim, hidden, page = 8, 2, 64, 768, 16
+    n, seqs = sum(qn), len(kv)
+    packed, full = zip(*(weight(r, c, i + 1) for i, (r, c) in enumerate([(heads * dim, hidden), (kv_heads * dim, hidden), (kv_heads * dim, hidden), (hidden, heads * dim)])))
+    g = torch.Generator().manual_seed(n)
+    need = [-(-x // page) for x in kv]
+    ids = torch.randperm(sum(need), generator=g).tolist()
+    table = [[ids.pop() if j < need[s] else -1 for j in range(max(need))] for s in range(seqs)]
+    start = [0] + np.cumsum(qn).tolist()
+    pool = torch.randn((2, sum(need), page, kv_heads, dim), generator=g)
+    scales = (None, None)
+    if kind == "e4m3":
+        scales = tuple(torch.full((kv_heads,), s, device=DEV) for s in (0.02, 0.03))
+        pool = (pool / 0.02).clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8)
+    else:
+        pool = pool.bfloat16()
+    pool = pool.to(DEV)
+    cache = ecfa.Cache(pool[0], pool[1], *scales)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    batch = ecfa.Batch(i32(table), i32(kv), i32(start), n, max(qn), max(kv))
+    freq, _ = ecfa.rope_freq(dim, 10000.0)
+    step = CompressedAttention(dict(zip("qkvo", packed)), heads, cache, batch, ecfa.Rope(freq))
+    x = torch.randn((n, hidden), generator=g).bfloat16().to(DEV)
+    y = step(x)
+    torch.cuda.synchronize()
+
+    assert close_quant(step.x8, step.x_scale, x)
+    for out, w in zip(step.group.y, full):
+        assert close_product(out, step.x8, step.x_scale, w)
+    toks = ref.tokens(start, kv, table, page, sum(need))
+    f = [int(v) % 2 ** 64 for v in freq.cpu().tolist()]
+    places = [t[1] for t in toks]
+    turned = ref.turned(step.q.cpu().double().numpy(), places, f, dim, False)
+    assert ref.near_bf16(step.turned.cpu().double().numpy(), turned, 2 * np.abs(turned).max(-1, keepdims=True)).all()
+    held = [ref.values(c, s) for c, s in ((cache.k, scales[0]), (cache.v, scales[1]))]
+    for new, c, s in ((ref.turned(step.k.cpu().double().numpy(), places, f, dim, False), held[0], scales[0]), (step.v.cpu().double().numpy(), held[1], scales[1])):
+        for t, (_, place, slots) in enumerate(toks):
+            most = 2 * np.abs(new[t]).max(-1, keepdims=True)
+            if kind == "bf16":
+                assert ref.near_bf16(c[slots[place]], new[t], most).all()
+            else:
+                by = s.cpu().double().numpy()[:, None]
+                limited = np.clip(new[t], -448 * by, 448 * by)
+                assert (np.abs(c[slots[place]] - limited) <= 2.0 ** -4 * np.abs(limited) + 2.0 ** -10 * by + 2.0 ** -18 * most).all()
+    want, size = ref.attend(step.turned, held[0], held[1], toks, dim ** -0.5)
+    assert (np.abs(step.seen.cpu().double().numpy() - want) <= ref.attend_bound(want, size)).all()
+    assert close_quant(step.seen8, step.seen_scale, step.seen)
+    assert y.data_ptr() == step.y.data_ptr() and close_product(y, step.seen8, step.seen_scale, full[3])
+
+    # captured once, replayed with other hidden states and lengths: the same as called
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(x)
+    for i in range(3):
+        x.copy_(torch.randn(x.shape, generator=g))
+        batch.kv_len.copy_(torch.tensor([max(m, l - i) for l, m in zip(kv, qn)], dtype=torch.int32))
+        kept = pool.clone()
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed, pool_then = step.y.clone(), pool.clone()
+        pool.copy_(kept)
+        step.y.zero_()
+        called = step(x)
+        torch.cuda.synchronize()
+        assert torch.equal(replayed, called) and torch.equal(pool_then.view(torch.uint8), pool.view(torch.uint8))
+
+
+def test_shapes_that_do_not_fit():
+    packed = {w: weight(256, 256, i)[0] for i, w in enumerate("qkvo")}
+    pool = torch.zeros((2, 4, 16, 2, 64), dtype=torch.bfloat16, device=DEV)
+    cache = ecfa.Cache(pool[0], pool[1])
+    zeros = torch.zeros((1, 4), dtype=torch.int32, device=DEV)
+    with pytest.raises(ecf8.Ecf8Error) as e:                     # k and v are of 2 heads of 64
+        CompressedAttention(packed, 4, cache, ecfa.Batch(zeros, zeros[0, :1]))
+    assert e.value.code == ecf8.E_ARG
+    packed.update({w: weight(128, 256, 7)[0] for w in "kv"})
+    CompressedAttention(packed, 4, cache, ecfa.Batch(zeros, zeros[0, :1]))
+    with pytest.raises(ecf8.Ecf8Error) as e:
+        CompressedAttention(packed, 4, cache, ecfa.Batch(zeros.expand(65, 4).contiguous(), torch.zeros(65, dtype=torch.int32, device=DEV)))
+    assert e.value.code == ecf8.E_ARG
