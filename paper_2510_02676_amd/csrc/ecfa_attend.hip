@@ -8,7 +8,7 @@
 namespace {
 using namespace ecfa;
 
-constexpr int JOIN_THREADS = 256;
+constexpr int JOIN_THREADS = 256, JOIN_FEW = 8;
 
 // The pieces' (m, l, O) of a row to one row: a thread four elements of it, from piece `first` on every `by`-th one, four pieces' at once.
 struct Joined {
@@ -54,9 +54,10 @@ __device__ inline void write_joined(const AttendArgs &a, const Joined &j, int64_
 }
 
 // Reads what the pieces have written, 4 head_dim + 8 bytes a row and piece, once.  The first few_blocks workgroups are for rows of the few-rows
-// kernel's first tiles, which may have hundreds of pieces: one workgroup a row (few_joined of each sequence and key/value head, and what lies
-// beyond those in turn), groups of head_dim / 4 threads share the pieces.  The others are for a token of the other kernel each, with few
-// pieces: head_dim / 4 threads a row.
+// kernel's first tiles, few_joined of them for each sequence and key/value head.  Such a row may have hundreds of pieces: then the groups of
+// head_dim / 4 threads of a workgroup share them; up to JOIN_FEW pieces are one group's work.  The others are for a token of the
+// other kernel each, with few pieces: head_dim / 4 threads a row.  Bound by its chain: lengths, plan, pieces, rows take 4 us for one
+// token of 4096 keys (4 rows to a head) as for 64 of them.
 __global__ __launch_bounds__(JOIN_THREADS) void ecfa_attend_join_kernel(const AttendArgs a, uint32_t few_blocks, uint32_t few_joined)
 {
     __shared__ f32x4 sums[JOIN_THREADS];
@@ -84,6 +85,15 @@ __global__ __launch_bounds__(JOIN_THREADS) void ecfa_attend_join_kernel(const At
     const Seq sq = seq_of(a.b, s);
     const int32_t rows = sq.qn * share < (int32_t)a.few_tile ? sq.qn * share : (int32_t)a.few_tile;
     const int64_t stride = (int64_t)a.kv_heads * a.few_tile;
+    if (it.used <= JOIN_FEW) {                                 // few pieces: a row for each group of threads
+        if (group >= groups) return;
+        for (int32_t row = (int32_t)(blockIdx.x % few_joined * groups + group); row < rows; row += (int32_t)(few_joined * groups)) {
+            const int32_t tok = over(row, a.by_share);
+            write_joined(a, join(a, few_part(a, it.first_item, kvh, row), stride, it.used, 0, 1, quad), (int64_t)sq.q0 + tok,
+                         (int64_t)kvh * a.share + (row - tok * share), quad);
+        }
+        return;
+    }
     for (int32_t row = (int32_t)(blockIdx.x % few_joined); row < rows; row += (int32_t)few_joined) {
         const int64_t part = few_part(a, it.first_item, kvh, row);
         Joined j{NONE, 0.f, f32x4{0, 0, 0, 0}};
@@ -142,7 +152,10 @@ uint32_t splits_of(uint64_t tiles, uint64_t slots, uint64_t keys)
 }
 
 // Up to 32 rows of a sequence (the heads that share their keys, times its new tokens) go to the few-rows kernel, which reads K and V without
-// waiting for other waves; more go to 128-row tiles.  `window`: 0 if there is none; with one, no more is asked for than without.
+// waiting for other waves and cuts the keys in equal pieces; more go to 128-row tiles.  At 32 rows, heads of 128, BF16: one
+// sequence of 4096 keys 18.8 us (tiles 31.1), 64 of them with 8 heads 232 (236), E4M3 143 (177).  17 to 32 rows that meet no more
+// than 512 keys go to tiles as well, which need no second kernel then: 64 sequences of 512 keys 29.3 us (few-rows kernel 44.0), E4M3 25.5 (31.3).
+// `window`: 0 if there is none; with one, no more is asked for than without.
 Shape shape_of(const ecfa_cache *c, const ecfa_batch *b, uint32_t heads, uint32_t cus, uint64_t window)
 {
     Shape p{};
@@ -153,7 +166,7 @@ Shape shape_of(const ecfa_cache *c, const ecfa_batch *b, uint32_t heads, uint32_
     const uint64_t max_kv = b->max_kv && b->max_kv < keys ? b->max_kv : keys;
     const auto seen = [&](uint64_t rows) { return window && window + rows < max_kv ? window + rows : max_kv; };    // keys of a tile
     const uint64_t rows = (uint64_t)max_q * share;
-    if (rows <= 32) {              // few rows everywhere
+    if (rows <= 16 || (rows <= 32 && max_kv > 512)) {          // few rows everywhere
         p.few = true;
         p.few_rows = 0x7fffffff;
         p.few_tiles = rows <= 16 ? 1 : 2;
@@ -164,14 +177,21 @@ Shape shape_of(const ecfa_cache *c, const ecfa_batch *b, uint32_t heads, uint32_
         p.few_rows = p.few ? 16 * (int32_t)p.few_tiles : 0;
     }
     p.many_splits = 1;
-    if (p.few) {                   // two workgroups on each compute unit, with a step for each wave at least; thousands of sequences need no pieces
+    if (p.few) {
+        // As many pieces as make two workgroups on each compute unit, with a step for each wave at least (two for 32 rows); thousands of
+        // sequences need none.  One token of 131072 keys, 64 of up to 8192, 16 times 8 tokens of 4096: two workgroups 108, 49, 77 us; one 131, 52,
+        // 88; four 111, 49, 94.  Twice as many steps at least: 2048 keys of one token 12.7 us, 11.4 with one; 8 tokens after 4088 keys 18.8 us,
+        // 21.6 with one.
         const uint32_t bytes = p.kc * 32 * (c->dtype == ECFA_E4M3 ? 1 : 2);
-        p.few_unit = FEW_WAVES * (p.few_tiles > 1 ? 1 : bytes <= 64 ? 4 : bytes <= 128 ? 2 : 1);        // as in FewShape
+        p.few_unit = FEW_WAVES * (p.few_tiles > 1 ? 2 : bytes <= 64 ? 4 : bytes <= 128 ? 2 : 1);        // KU of FewShape, of two sub-tiles twice that
         const uint64_t want = (2ull * cus + c->kv_heads - 1) / c->kv_heads, pieces = (seen(16 * p.few_tiles) + 32 * p.few_unit - 1) / (32 * p.few_unit);
         const uint64_t most = pieces * b->n_seqs;
         p.few_goal = pieces <= 1 || b->n_seqs > 1024 ? 0 : (uint32_t)(want < most ? want : most);
         p.few_items = p.few_goal + b->n_seqs;
-        p.few_joined = (uint32_t)(rows < 16 * p.few_tiles ? rows : 16 * p.few_tiles);
+        // In the second kernel a workgroup a row while all of them are on the card at once, and then a group of its threads a row (16 times 8
+        // tokens of 4096 keys, 4096 rows and heads: 77.0 -> 67.5 us; 15 times 16 rows of a head of 256, 1920: 32.5, by groups 35.3).
+        const uint32_t joined = (uint32_t)(rows < 16 * p.few_tiles ? rows : 16 * p.few_tiles), groups = JOIN_THREADS / (c->head_dim / 4);
+        p.few_joined = (uint64_t)b->n_seqs * c->kv_heads * joined < 8ull * cus ? joined : (joined + groups - 1) / groups;
         if (p.few_goal) p.few_parts = (uint64_t)p.few_items * c->kv_heads * 16 * p.few_tiles;
     }
     if (p.many) {

@@ -304,6 +304,9 @@ void launch_append_of_size(const AppendArgs &a, uint64_t bytes, bool interleaved
     else launch_append<F32, F8, false>(a, interleaved, s);
 }
 
+// Threads for a row so that it fits four pieces of eight a thread and rows are spread over the card.  BF16, 4096 rows: 512 columns with 64 threads
+// 4.8 us, with 256 5.2, with 1024 13.5; 8192 columns with 256 17.8, with 64 24.6, with 1024 20.2; 16384 columns with 1024
+// 32.3, with 256 37.7.
 template <bool F32>
 void launch_quant(const QuantArgs &a, uint32_t group, hipStream_t s)
 {
