@@ -132,7 +132,7 @@ struct Shape {
 // last workgroup end first: rounds of two workgroups on each compute unit (one for heads of more than 128 elements, by registers), each
 // the steps of 64 keys of a piece and a start of about four steps' time; for the second kernel as much again, and a little for each piece.
 // (192 tiles of 8768 keys: 5 pieces 136 us, 3 pieces 160; 300 tiles of 9200: 3 pieces 204, 2 pieces 234.)  More tiles than
-// that are of unlike length and fill one another's gaps (512 tiles of 10240 keys: whole 255 us, in two 272).
+// that are of unlike length and fill one another's gaps (512 tiles of 8192 keys: whole 255 us, in two 272).
 uint32_t splits_of(uint64_t tiles, uint64_t slots, uint64_t keys)
 {
     if (tiles > slots || keys <= 512) return 1;

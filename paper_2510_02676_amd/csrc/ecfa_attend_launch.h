@@ -6,7 +6,8 @@
 namespace ecfa {
 
 // Chunks and single tokens of one step in one launch: the tiles of many rows first, which take longest, then the items of few rows, which fill
-// compute units as they come free.
+// compute units as they come free.  13 sequences of 1 to 517 tokens, window 1000, scores capped, E4M3: 50 us with the second
+// kernel where two launches, and a workgroup for each row that is joined, took 75.  The items first: 2 us more.
 template <int KC, bool F8, bool EXTRA>
 __global__ __launch_bounds__(256, KC <= 4 ? 2 : 1) void ecfa_attend_mixed_kernel(const AttendArgs a, uint32_t many_blocks)
 {
@@ -19,7 +20,7 @@ __global__ __launch_bounds__(256, KC <= 4 ? 2 : 1) void ecfa_attend_mixed_kernel
 template <int KC, bool F8>
 int launch_attend_kc(const AttendArgs &a, bool few, bool many, hipStream_t s)
 {
-    // Caps and slopes in instances of their own: with them in every one 4680 x 4680 tokens took 593 us, without 484.
+    // Caps and slopes in instances of their own: with them in every one 4680 x 4680 tokens of 40 heads took 593 us, without 484.
     const bool extra = a.cap > 0.f || a.slopes;
     const uint32_t few_blocks = a.few_items * a.kv_heads, many_blocks = a.many_tiles * a.kv_heads * a.many_splits;
     if (few && many && a.few_tile == 16) {
