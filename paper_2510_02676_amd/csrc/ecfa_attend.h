@@ -224,7 +224,8 @@ __device__ inline float sum_xor(float x)
 
 // The score of a dot product x, in units of ln 2, with the cap if there is one: softcap * tanh(y), y = scale x / softcap, and
 // tanh(y) = 1 - 2 / (e^(2 y) + 1), which is off by 2^-23 of the cap at most.  That is all for caps up to SIMPLE_CAP (2^-16 of a score); beyond
-// it small y, where that loses digits, take y - y^3 / 3 + 2 y^5 / 15 (error below 2^-26 |y| for |y| < 0.06).  cap_in = to_log2 * 2 / softcap.
+// it small y, where that loses digits, take y - y^3 / 3 + 2 y^5 / 15 (error below 2^-26 |y| for |y| < 0.06),
+// which costs 6 % of a mixed batch whose scores are capped (47.4 -> 50.3 us).  cap_in = to_log2 * 2 / softcap.
 constexpr float SIMPLE_CAP = 64.f;
 __device__ inline float capped_or_scaled(const AttendArgs &a, float x, float to_log2, float cap_in)
 {

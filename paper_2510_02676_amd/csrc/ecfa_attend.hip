@@ -56,8 +56,8 @@ __device__ inline void write_joined(const AttendArgs &a, const Joined &j, int64_
 // Reads what the pieces have written, 4 head_dim + 8 bytes a row and piece, once.  The first few_blocks workgroups are for rows of the few-rows
 // kernel's first tiles, few_joined of them for each sequence and key/value head.  Such a row may have hundreds of pieces: then the groups of
 // head_dim / 4 threads of a workgroup share them; up to JOIN_FEW pieces are one group's work.  The others are for a token of the
-// other kernel each, with few pieces: head_dim / 4 threads a row.  Bound by its chain: lengths, plan, pieces, rows take 4 us for one
-// token of 4096 keys (4 rows to a head) as for 64 of them.
+// other kernel each, with few pieces: head_dim / 4 threads a row.  Bound by its chain: lengths, plan, pieces, rows take 4.9 us for one
+// token of 4096 keys and 5.9 for 64 of up to 8192.
 __global__ __launch_bounds__(JOIN_THREADS) void ecfa_attend_join_kernel(const AttendArgs a, uint32_t few_blocks, uint32_t few_joined)
 {
     __shared__ f32x4 sums[JOIN_THREADS];

@@ -23,6 +23,7 @@ struct CacheView {                           // strides in bytes
     int64_t k_page, k_tok, k_head, v_page, v_tok, v_head;
     uint32_t n_pages, page_shift;
     uint32_t near;                           // tokens of a page lie less than 2^25 bytes apart: offsets over 16 of them fit 32 bits
+                                             // (2048 tokens of 8192 keys 262 us, with an address a lane 286; 131072 keys 109.4, 111.2)
 };
 
 struct BatchView {
