@@ -32,11 +32,20 @@ __device__ inline int spread(int r)
 
 // The first tile of a sequence among all tiles of the launch: rows before it, in whole tiles, and one more for each sequence before it,
 // which is never less than they need.
-__device__ inline uint32_t first_tile(const AttendArgs &a, uint32_t s)
+__host__ __device__ inline uint32_t first_tile(const AttendArgs &a, uint32_t s)
 {
     int32_t x = a.b.q_start ? a.b.q_start[s] : (int32_t)s;
     x = x < 0 ? 0 : x > (int32_t)a.b.n_tokens ? (int32_t)a.b.n_tokens : x;
     return (uint32_t)((uint64_t)x * a.share / MANY_ROWS) + s;
+}
+
+// The row of sequence s, of `rows`, that a tile of the launch begins with, or -1: behind the sequence's last row, or before its first tile.
+// The latter is what tiles before the first sequence have where the first start is above 0 (the search gives them sequence 0).
+__host__ __device__ inline int32_t first_row(const AttendArgs &a, uint32_t s, uint32_t tile, int32_t rows)
+{
+    const uint32_t first = first_tile(a, s);
+    const uint64_t row = (uint64_t)(tile - first) * MANY_ROWS;
+    return tile < first || row >= (uint64_t)rows ? -1 : (int32_t)row;
 }
 
 __device__ inline uint32_t seq_of_tile(const AttendArgs &a, uint32_t tile)     // as seq_of_row
@@ -73,8 +82,8 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, uint32_t block,
     const Seq sq = seq_of(a.b, s);
     const int32_t rows = sq.qn * (int32_t)a.share;
     if (rows <= a.few_rows) return;                            // the other kernel's
-    const int32_t row0 = (int32_t)(at - first_tile(a, s)) * MANY_ROWS;
-    if (row0 >= rows) return;
+    const int32_t row0 = first_row(a, s, at, rows);
+    if (row0 < 0) return;
     const int32_t row_end = row0 + MANY_ROWS < rows ? row0 + MANY_ROWS : rows;
     const int32_t prefix = prefix_of(a, s, sq);
     const int32_t share = (int32_t)a.share;

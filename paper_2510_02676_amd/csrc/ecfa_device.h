@@ -39,7 +39,7 @@ struct Seq {
     int32_t len;                             // keys that the table has room for
 };
 
-__device__ inline Seq seq_of(const BatchView &b, uint32_t s)
+__host__ __device__ inline Seq seq_of(const BatchView &b, uint32_t s)
 {
     Seq r;
     int32_t kv = b.kv_len[s];

@@ -449,3 +449,33 @@ def test_counts_that_a_launch_cannot_hold():
     with pytest.raises(ecf8.Ecf8Error) as e:                     # 2^27 workgroups
         ecfa.ecfa_attend(ecfa.Cache(heads[0], heads[1]), many, q, out=q)
     assert e.value.code == ecf8.E_ARG
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("kv,qn", [([3, 400], [200, 200]), ([3, 3000], [200, 200]), ([3, 420, 7, 300, 90], [130, 260, 1, 2, 70]), ([3, 2600, 1, 1900], [260, 50, 1, 40])])
+def test_rows_before_the_first_sequence(cache, kv, qn):
+    """Starts that begin above 0: the rows before them belong to nobody, whole tiles of them; keys cut in pieces and not, with single tokens and
+    without."""
+    s = Setting(kv, qn, cache=cache, seed=len(kv))
+    want, size = s.want()
+    whole = s.batch()
+    b = ecfa.Batch(whole.page_table[1:], whole.kv_len[1:].contiguous(), whole.q_start[1:].contiguous(), n_tokens=s.q_start[-1], max_q=max(qn[1:]), max_kv=max(kv))
+    q = s.q.to(DEV)
+    out = torch.full((q.shape[0] + 2, *q.shape[1:]), 7.0, dtype=torch.bfloat16, device=DEV)
+    ecfa.ecfa_attend(s.device_cache(), b, q, out=out[1:-1])
+    torch.cuda.synchronize()
+    got, first = out.cpu().double().numpy(), qn[0]
+    assert (got[:first + 1] == 7).all() and (got[-1] == 7).all()
+    assert (np.abs(got[1:-1] - want) <= ref.attend_bound(want, size))[first:].all()
+
+
+@pytest.mark.parametrize("max_kv", [400, 3000])
+def test_starts_that_are_wrong_stay_inside_with_many_rows(max_kv):
+    s = Setting([max_kv, 300, 40], [200, 100, 100], heads=16, kv_heads=2)
+    q, out = s.q.to(DEV), torch.full((402, 16, 128), 7.0, dtype=torch.bfloat16, device=DEV)
+    for starts in ([200, 400, 400, 400], [399, 400, 1000, 2000], [-5, 200, 300, 400], [300, 100, 400, 50], [0, 2 ** 30, -2 ** 30, 400], [2 ** 31 - 1, 0, 400, 400], [128, 64, 32, 0]):
+        b = s.batch()
+        b.q_start.copy_(torch.tensor(starts, dtype=torch.int32))
+        ecfa.ecfa_attend(s.device_cache(), b, q, out=out[1:401])
+        torch.cuda.synchronize()
+        assert (out[0] == 7).all() and (out[401] == 7).all()
