@@ -3,6 +3,9 @@
 Argument marshalling only; every step runs inside ``libecf8.so`` (importing this module fails loudly when the library is
 not built).  The objects here hold the C structures and keep the tensors they point to alive: a ``Cache`` and a ``Batch`` are
 made once and used by every layer's and every step's calls; the tensors inside them may be rewritten in place.
+
+A call on another stream than the current one (`stream`) makes what it allocates of that stream's memory; the caller orders that stream
+behind what wrote the call's inputs, and whatever reads the results behind that stream.
 """
 import ctypes
 
@@ -78,6 +81,17 @@ def _scale_ptr(t, heads):
     return t.data_ptr()
 
 
+def _empty(shape, dtype, device, stream):
+    """Memory for a call on `stream` (None: the current one).  It comes from that stream's own: a block of the current stream's may still be in use by
+    kernels queued there, which nothing orders `stream` behind.  The current stream is noted as a user of it, for the program that gets it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        x = torch.empty(shape, dtype=dtype, device=device)
+    x.record_stream(torch.cuda.current_stream(device))
+    return x
+
+
 class Cache:
     """A pool of pages: k and v are (pages, page_size, kv_heads, head_dim) tensors of BF16 or E4M3 (``torch.float8_e4m3fn``, or uint8
     holding its bytes), of any strides over the first three dimensions; k_scale and v_scale (kv_heads,) fp32 or None."""
@@ -147,7 +161,7 @@ def ecfa_append(cache, batch, k=None, v=None, q=None, q_out=None, rope=None, str
     if q is not None:
         rq = _rows("ecfa_append", q, n, 0, dim)
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+            q_out = _empty(q.shape, torch.bfloat16, q.device, stream)
         ro = _rows("ecfa_append", q_out, n, q.shape[1], dim)
     elif q_out is not None:
         raise _bad("ecfa_append")
@@ -157,11 +171,11 @@ def ecfa_append(cache, batch, k=None, v=None, q=None, q_out=None, rope=None, str
     return q_out
 
 
-def attend_workspace(cache, batch, heads):
-    """A workspace for ``ecfa_attend`` with `heads` query heads on this batch (a uint8 tensor, for one call at a time), or None if the calls
-    need none."""
+def attend_workspace(cache, batch, heads, stream=None):
+    """A workspace for ``ecfa_attend`` with `heads` query heads on this batch (a uint8 tensor, for one call at a time, on `stream`), or None if the
+    calls need none."""
     n = int(_lib.ecfa_attend_workspace_bytes(cache.c, batch.c, heads))
-    return torch.empty(n, dtype=torch.uint8, device=cache.device) if n else None
+    return _empty(n, torch.uint8, cache.device, stream) if n else None
 
 
 def ecfa_attend(cache, batch, q, scale=None, causal=True, window=0, softcap=0.0, slopes=None, prefix=None, out=None, workspace=None, stream=None):
@@ -171,14 +185,12 @@ def ecfa_attend(cache, batch, q, scale=None, causal=True, window=0, softcap=0.0,
     rq = _rows("ecfa_attend", q, n, 0, dim)
     heads = q.shape[1]
     if out is None:
-        out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+        out = _empty(q.shape, torch.bfloat16, q.device, stream)
     ro = _rows("ecfa_attend", out, n, heads, dim)
     if slopes is not None and (slopes.dtype != torch.float32 or slopes.shape != (heads,) or not slopes.is_contiguous()):
         raise _bad("ecfa_attend")
     if workspace is None:
-        workspace = attend_workspace(cache, batch, heads)
-        if workspace is not None and stream is not None:
-            workspace.record_stream(stream)
+        workspace = attend_workspace(cache, batch, heads, stream)
     opts = _AttendOpts(dim ** -0.5 if scale is None else scale, softcap, None if slopes is None else slopes.data_ptr(),
                        None if prefix is None else _i32("ecfa_attend", prefix, batch.kv_len.shape), int(causal), window)
     rc = _attend(cache.c, batch.c, opts, rq, ro, None if workspace is None else workspace.data_ptr(),
@@ -200,9 +212,9 @@ def ecfa_quant(x, group=0, q=None, scale=None, stream=None):
         raise _bad("ecfa_quant")
     want = (rows, cols // 128) if group else (rows,)
     if q is None:
-        q = torch.empty((rows, cols), dtype=torch.float8_e4m3fn, device=x.device)
+        q = _empty((rows, cols), torch.float8_e4m3fn, x.device, stream)
     if scale is None:
-        scale = torch.empty(want, dtype=torch.float32, device=x.device)
+        scale = _empty(want, torch.float32, x.device, stream)
     if (q.dtype not in _BYTES or q.shape != shape or not q.is_contiguous() or scale.dtype != torch.float32 or scale.shape != want
             or not scale.is_contiguous()):
         raise _bad("ecfa_quant")

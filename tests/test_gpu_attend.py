@@ -479,3 +479,41 @@ def test_starts_that_are_wrong_stay_inside_with_many_rows(max_kv):
         ecfa.ecfa_attend(s.device_cache(), b, q, out=out[1:401])
         torch.cuda.synchronize()
         assert (out[0] == 7).all() and (out[401] == 7).all()
+
+
+def test_memory_of_a_call_on_another_stream(monkeypatch):
+    """What a call allocates for another stream is no block that the current stream has just let go, whose kernels may still be using it."""
+    s = Setting([5000], [1], single=True)
+    cache, b, q = s.device_cache(), s.batch(), s.q.to(DEV)
+    k, v = (torch.zeros((1, 2, 128), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    side, given, attend = torch.cuda.Stream(), [], ecfa._attend
+    monkeypatch.setattr(ecfa, "_attend", lambda *a: given.append(a[5]) or attend(*a))
+    x = torch.randn((4, 1024), device=DEV)
+    torch.cuda.synchronize()
+    for call in (lambda stream: ecfa.ecfa_attend(cache, b, q, stream=stream), lambda stream: ecfa.ecfa_append(cache, b, k, v, q, stream=stream),
+                 lambda stream: ecfa.ecfa_quant(x, stream=stream), lambda stream: ecfa.ecfa_quant(x, 128, stream=stream)):
+        for _ in range(3):
+            given.clear()
+            mine = call(None)
+            held = {y.data_ptr() for y in (mine if isinstance(mine, tuple) else (mine,))} | {p for p in given if p}
+            given.clear()
+            del mine
+            other = call(side)
+            got = {y.data_ptr() for y in (other if isinstance(other, tuple) else (other,))} | {p for p in given if p}
+            assert not held & got
+            torch.cuda.synchronize()
+
+
+def test_calls_in_flight_on_two_streams():
+    """Unlike inputs, no buffers given: each gets its own result, whichever runs first."""
+    made = [(Setting([5000 + 64 * i], [1], single=True, seed=i), ) for i in range(4)]
+    made = [(s.device_cache(), s.batch(), s.q.to(DEV)) for s, in made]
+    want = [ecfa.ecfa_attend(*m) for m in made]
+    side, busy = torch.cuda.Stream(), torch.randn((4096, 4096), device=DEV)
+    torch.cuda.synchronize()
+    for _ in range(5):
+        busy @ busy                                              # what is queued here comes later than what is queued there
+        got = [ecfa.ecfa_attend(*m, stream=side if i % 2 else None) for i, m in enumerate(made * 3)]
+        torch.cuda.synchronize()
+        for i, y in enumerate(got):
+            assert torch.equal(y, want[i % 4])
