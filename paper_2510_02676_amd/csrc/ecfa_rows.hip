@@ -72,6 +72,23 @@ __device__ inline u32x2 pack8_e4m3(const float *x)
     return u32x2{(uint32_t)lo, (uint32_t)hi};
 }
 
+// x / by as E4M3 sees it: the fp32 quotient wherever it decides about the byte.  The product with the reciprocal alone would lose ties.  It is put
+// right by what is left of x: with r the reciprocal to the nearest and q within a unit of the quotient, q + (x - q by) r in two fused
+// operations is the quotient to the nearest (Markstein, 1990), as long as x - q by is a number of fp32, which scales from 2^-90 on see to for
+// quotients from 2^-11 on.  Smaller ones are zeros of their sign, larger ones than 1024 and infinities are limited.  Other scales: divisions.
+// 6472 tokens, BF16 rows, 32 + 2 x 8 heads of 128: 24.0 us, with sixteen divisions 26.0, with the product alone 23.5.
+__device__ inline void divide16_e4m3(float *x, float by)
+{
+    if (by >= 0x1p-90f && by <= 0x1p90f) {
+        const float r = 1.f / by;
+        for (int j = 0; j < 16; j++) {
+            const float q = x[j] * r, y = __builtin_fmaf(__builtin_fmaf(-q, by, x[j]), r, q);
+            x[j] = __builtin_fabsf(q) < 1024.f ? __builtin_copysignf(y, q) : q;
+        }
+    } else
+        for (int j = 0; j < 16; j++) x[j] /= by;
+}
+
 // A workgroup takes one token.  A thread keeps its 16 elements' place within a head (eight pairs: 8 u .. and rot / 2 + 8 u .. by
 // halves, 16 u .. interleaved) and walks over the heads of q, k and v, so that its eight sines and cosines are made once.  The angle
 // is position times frequency modulo 2^64 of a turn: the upper 32 bits go to the sine unit, which takes turns, and the
@@ -142,8 +159,8 @@ __global__ __launch_bounds__(APPEND_THREADS) void ecfa_append_kernel(const Appen
                             : a.c.k + (int64_t)page * a.c.k_page + (int64_t)at * a.c.k_tok + (int64_t)hh * a.c.k_head;
         const float *scales = is_v ? a.c.v_scale : a.c.k_scale;
         if (scales) {
-            const float inv = 1.f / scales[hh];
-            for (int j = 0; j < 16; j++) x[j] *= inv;
+            if constexpr (F8) divide16_e4m3(x, scales[hh]);
+            else for (int j = 0; j < 16; j++) x[j] /= scales[hh];
         }
         if constexpr (F8) {
             put<PAST>(dst + d0 * DST, pack8_e4m3(x));

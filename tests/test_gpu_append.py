@@ -274,3 +274,47 @@ def test_refusals_on_the_device_side_of_the_binding():
     for bad in (x.half(), x.t(), x[:, 1:], x[:, :200]):
         with pytest.raises(ecf8.Ecf8Error):
             ecfa.ecfa_quant(bad)
+
+
+def e4m3_bytes(y):
+    """fp32 numbers as E4M3 bytes, limited to 448, to the nearest, ties to the even byte."""
+    value = ref.E4M3[:127]
+    y = y.astype(np.float64)
+    size = np.minimum(np.abs(y), 448.0)
+    between = (value[1:] + value[:-1]) / 2
+    below = np.searchsorted(between, size, side="left")          # between[below - 1] < size <= between[below]
+    tie = (below < 126) & (size == between[np.minimum(below, 125)])
+    return np.where(tie & (below % 2 == 1), below + 1, below).astype(np.uint8) | np.where(np.signbit(y), 128, 0).astype(np.uint8)
+
+
+@pytest.mark.parametrize("src", [torch.float32, torch.bfloat16])
+def test_e4m3_is_of_the_quotient_by_the_scale(src):
+    """Numbers whose quotient by the scale is a tie of E4M3, and their neighbours, by scales that are no powers of two; and scales that have no
+    reciprocal in fp32, denormals among them: the bytes are those of the fp32 quotient."""
+    value = ref.E4M3[:127]
+    ties = np.concatenate([(value[1:] + value[:-1]) / 2, [0.0, 448.0, 464.0]])
+    scales = np.array([0.0123, 0.3, 7.7, 1.0 / 3.0, 2.0 ** -128, 2.0 ** -129 * 1.25, 1e-42, 1e-30, 2.0 ** -90 * 1.1, 2.0 ** -90 * 0.9, 8e26, 2.0 ** 90 * 1.7], dtype=np.float32)
+    near = []
+    for by in scales:
+        x = (ties * float(by)).astype(np.float32)
+        if src == torch.bfloat16:
+            x = torch.from_numpy(x).bfloat16().float().numpy()
+        else:
+            bits = np.minimum(x.view(np.int32)[:, None] + np.arange(-4, 5, dtype=np.int32), 0x7f000000)
+            x = np.maximum(bits, 0).view(np.float32).ravel()
+        near.append(np.concatenate([x, -x]))
+    near = np.stack(near)                                        # (heads, numbers)
+    near = np.pad(near, ((0, 0), (0, -near.shape[1] % 128))).reshape(len(scales), -1, 128).transpose(1, 0, 2).copy()
+    n = near.shape[0]
+    want = e4m3_bytes(np.divide(near, scales[:, None], dtype=np.float32))
+    if src == torch.float32:                                     # (what a reciprocal would give is something else)
+        with np.errstate(over="ignore", invalid="ignore", divide="ignore"):
+            other = near * (np.float32(1) / scales)[:, None]
+        assert (e4m3_bytes(np.nan_to_num(other)) != want).sum() > 100
+    x = torch.from_numpy(near).to(src).to(DEV)
+    pool = torch.zeros((2, -(-n // 16), 16, len(scales), 128), dtype=torch.uint8, device=DEV)
+    by = torch.from_numpy(scales).to(DEV)
+    b = ecfa.Batch(torch.arange(pool.shape[1], dtype=torch.int32, device=DEV)[None], i32([n]), i32([0, n]), n_tokens=n)
+    ecfa.ecfa_append(ecfa.Cache(pool[0], pool[1], by, by), b, x, -x)
+    got = pool.view(2, -1, len(scales), 128)[:, :n].cpu().numpy()
+    assert np.array_equal(got[0], want) and np.array_equal(got[1], want ^ 128)
