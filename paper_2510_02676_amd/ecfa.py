@@ -5,7 +5,8 @@ not built).  The objects here hold the C structures and keep the tensors they po
 made once and used by every layer's and every step's calls; the tensors inside them may be rewritten in place.
 
 A call on another stream than the current one (`stream`) makes what it allocates of that stream's memory; the caller orders that stream
-behind what wrote the call's inputs, and whatever reads the results behind that stream.
+behind what wrote the call's inputs, and whatever reads the results behind that stream.  All tensors of a call are on one device, that of its
+stream, or it is refused (``E_ARG``).
 """
 import ctypes
 
@@ -59,24 +60,36 @@ def _bad(fn):
     return _e.Ecf8Error(fn, _e.E_ARG)
 
 
-def _rows(fn, x, n_tokens, heads, dim):
+def _stream_ptr(fn, on, stream):
+    """The stream's handle, for tensors on the device of number `on` (-1, the host, is nobody's): it has to be one of that device's."""
+    if stream is not None:
+        if stream.device_index != on:
+            raise _bad(fn)
+    elif on < 0 or torch.cuda.current_device() != on:
+        raise _bad(fn)
+    elif _e._raw_stream is not None:
+        return _e._raw_stream(on)
+    return _e._stream_ptr(stream)
+
+
+def _rows(fn, x, n_tokens, heads, dim, on):
     """A (tokens, heads, dim) tensor as the C structure: any strides, elements of a head next to each other."""
     shape, stride, dtype = x.shape, x.stride(), _DTYPE.get(x.dtype)
-    if len(shape) != 3 or shape[0] != n_tokens or shape[2] != dim or (heads and shape[1] != heads) or dtype is None or stride[2] != 1:
+    if len(shape) != 3 or shape[0] != n_tokens or shape[2] != dim or (heads and shape[1] != heads) or dtype is None or stride[2] != 1 or x.get_device() != on:
         raise _bad(fn)
     return _Rows(x.data_ptr(), stride[0], stride[1], shape[1], dtype)
 
 
-def _i32(fn, t, shape):
-    if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous():
+def _i32(fn, t, shape, on):
+    if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous() or t.get_device() != on:
         raise _bad(fn)
     return t.data_ptr()
 
 
-def _scale_ptr(t, heads):
+def _scale_ptr(t, heads, on):
     if t is None:
         return None
-    if t.dtype != torch.float32 or t.shape != (heads,) or not t.is_contiguous():
+    if t.dtype != torch.float32 or t.shape != (heads,) or not t.is_contiguous() or t.get_device() != on:
         raise _bad("Cache")
     return t.data_ptr()
 
@@ -97,7 +110,7 @@ class Cache:
     holding its bytes), of any strides over the first three dimensions; k_scale and v_scale (kv_heads,) fp32 or None."""
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
-        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.stride(3) != 1 or v.stride(3) != 1:
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.stride(3) != 1 or v.stride(3) != 1 or k.get_device() != v.get_device():
             raise _bad("Cache")
         if k.dtype == torch.bfloat16:
             dtype = BF16
@@ -107,7 +120,8 @@ class Cache:
             raise _bad("Cache")
         pages, page, heads, dim = k.shape
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.c = _Cache(k.data_ptr(), v.data_ptr(), _scale_ptr(k_scale, heads), _scale_ptr(v_scale, heads), (_i64 * 3)(*k.stride()[:3]),
+        self.on = k.get_device()
+        self.c = _Cache(k.data_ptr(), v.data_ptr(), _scale_ptr(k_scale, heads, self.on), _scale_ptr(v_scale, heads, self.on), (_i64 * 3)(*k.stride()[:3]),
                         (_i64 * 3)(*v.stride()[:3]), pages, page, heads, dim, dtype, 0)
         self.kv_heads, self.head_dim, self.device = heads, dim, k.device
 
@@ -127,7 +141,8 @@ class Batch:
             n_tokens = seqs
         self.page_table, self.kv_len, self.q_start = page_table, kv_len, q_start
         self.n_tokens = n_tokens
-        self.c = _Batch(page_table.data_ptr(), _i32("Batch", kv_len, (seqs,)), None if q_start is None else _i32("Batch", q_start, (seqs + 1,)),
+        self.on = page_table.get_device()
+        self.c = _Batch(page_table.data_ptr(), _i32("Batch", kv_len, (seqs,), self.on), None if q_start is None else _i32("Batch", q_start, (seqs + 1,), self.on),
                         page_table.stride(0), width, seqs, n_tokens, max_q, max_kv, 0)
 
 
@@ -146,26 +161,28 @@ class Rope:
         if freq.dim() != 1 or freq.dtype != torch.int64 or not freq.is_contiguous():
             raise _bad("Rope")
         self.freq, self.pos = freq, pos
-        self.c = _Rope(freq.data_ptr(), None if pos is None else _i32("Rope", pos, pos.shape), 2 * freq.numel(), int(interleaved), scale, 0)
+        self.on = freq.get_device()
+        self.c = _Rope(freq.data_ptr(), None if pos is None else _i32("Rope", pos, pos.shape, self.on), 2 * freq.numel(), int(interleaved), scale, 0)
 
 
 def ecfa_append(cache, batch, k=None, v=None, q=None, q_out=None, rope=None, stream=None):
     """k turned and v into the cache, q turned into q_out (allocated if absent), which is returned.  k, v: (n_tokens, kv_heads,
     head_dim), q: (n_tokens, heads, head_dim), all fp32 or all BF16."""
-    n, dim = batch.n_tokens, cache.head_dim
-    if rope is not None and rope.pos is not None and rope.pos.numel() != n:
+    n, dim, on = batch.n_tokens, cache.head_dim, cache.on
+    if batch.on != on or (rope is not None and (rope.on != on or (rope.pos is not None and rope.pos.numel() != n))):
         raise _bad("ecfa_append")
-    rk = None if k is None else _rows("ecfa_append", k, n, cache.kv_heads, dim)
-    rv = None if v is None else _rows("ecfa_append", v, n, cache.kv_heads, dim)
+    at = _stream_ptr("ecfa_append", on, stream)
+    rk = None if k is None else _rows("ecfa_append", k, n, cache.kv_heads, dim, on)
+    rv = None if v is None else _rows("ecfa_append", v, n, cache.kv_heads, dim, on)
     rq = ro = None
     if q is not None:
-        rq = _rows("ecfa_append", q, n, 0, dim)
+        rq = _rows("ecfa_append", q, n, 0, dim, on)
         if q_out is None:
             q_out = _empty(q.shape, torch.bfloat16, q.device, stream)
-        ro = _rows("ecfa_append", q_out, n, q.shape[1], dim)
+        ro = _rows("ecfa_append", q_out, n, q.shape[1], dim, on)
     elif q_out is not None:
         raise _bad("ecfa_append")
-    rc = _append(cache.c, batch.c, None if rope is None else rope.c, rq, rk, rv, ro, _e._stream_ptr(stream))
+    rc = _append(cache.c, batch.c, None if rope is None else rope.c, rq, rk, rv, ro, at)
     if rc:
         _e._check("ecfa_append", rc)
     return q_out
@@ -181,20 +198,25 @@ def attend_workspace(cache, batch, heads, stream=None):
 def ecfa_attend(cache, batch, q, scale=None, causal=True, window=0, softcap=0.0, slopes=None, prefix=None, out=None, workspace=None, stream=None):
     """Attention of the batch's new tokens over the cache; q and the result (n_tokens, heads, head_dim) BF16.  scale defaults to
     head_dim^-0.5; slopes (heads,) fp32; prefix (seqs,) int32.  Without a workspace one is allocated for the call where it needs it."""
-    n, dim = batch.n_tokens, cache.head_dim
-    rq = _rows("ecfa_attend", q, n, 0, dim)
+    n, dim, on = batch.n_tokens, cache.head_dim, cache.on
+    if batch.on != on:
+        raise _bad("ecfa_attend")
+    at = _stream_ptr("ecfa_attend", on, stream)
+    rq = _rows("ecfa_attend", q, n, 0, dim, on)
     heads = q.shape[1]
     if out is None:
         out = _empty(q.shape, torch.bfloat16, q.device, stream)
-    ro = _rows("ecfa_attend", out, n, heads, dim)
-    if slopes is not None and (slopes.dtype != torch.float32 or slopes.shape != (heads,) or not slopes.is_contiguous()):
+    ro = _rows("ecfa_attend", out, n, heads, dim, on)
+    if slopes is not None and (slopes.dtype != torch.float32 or slopes.shape != (heads,) or not slopes.is_contiguous() or slopes.get_device() != on):
         raise _bad("ecfa_attend")
     if workspace is None:
         workspace = attend_workspace(cache, batch, heads, stream)
+    elif workspace.get_device() != on or not workspace.is_contiguous():
+        raise _bad("ecfa_attend")
     opts = _AttendOpts(dim ** -0.5 if scale is None else scale, softcap, None if slopes is None else slopes.data_ptr(),
-                       None if prefix is None else _i32("ecfa_attend", prefix, batch.kv_len.shape), int(causal), window)
+                       None if prefix is None else _i32("ecfa_attend", prefix, batch.kv_len.shape, on), int(causal), window)
     rc = _attend(cache.c, batch.c, opts, rq, ro, None if workspace is None else workspace.data_ptr(),
-                 0 if workspace is None else workspace.numel(), _e._stream_ptr(stream))
+                 0 if workspace is None else workspace.numel(), at)
     if rc:
         _e._check("ecfa_attend", rc)
     return out
@@ -207,6 +229,8 @@ def ecfa_quant(x, group=0, q=None, scale=None, stream=None):
     if len(shape) != 2 or dtype is None or group not in (0, 128):
         raise _bad("ecfa_quant")
     rows, cols = shape
+    on = x.get_device()
+    at = _stream_ptr("ecfa_quant", on, stream)
     row_stride, one = x.stride()
     if cols > 1 and one != 1:
         raise _bad("ecfa_quant")
@@ -216,9 +240,9 @@ def ecfa_quant(x, group=0, q=None, scale=None, stream=None):
     if scale is None:
         scale = _empty(want, torch.float32, x.device, stream)
     if (q.dtype not in _BYTES or q.shape != shape or not q.is_contiguous() or scale.dtype != torch.float32 or scale.shape != want
-            or not scale.is_contiguous()):
+            or not scale.is_contiguous() or q.get_device() != on or scale.get_device() != on):
         raise _bad("ecfa_quant")
-    rc = _quant(x.data_ptr(), dtype, rows, cols, row_stride, group, q.data_ptr(), scale.data_ptr(), _e._stream_ptr(stream))
+    rc = _quant(x.data_ptr(), dtype, rows, cols, row_stride, group, q.data_ptr(), scale.data_ptr(), at)
     if rc:
         _e._check("ecfa_quant", rc)
     return q, scale

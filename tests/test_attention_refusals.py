@@ -161,3 +161,22 @@ def test_the_binding_checks_what_it_is_given():
         ecfa.ecfa_append(c, b, t(2, 2, 64), t(2, 2, 64), q_out=t(2, 4, 64))
     with pytest.raises(ecf8.Ecf8Error):
         ecfa.ecfa_append(c, b, t(2, 2, 64), t(2, 2, 64), rope=ecfa.Rope(torch.zeros(32, dtype=torch.int64), pos=i32(3)))
+
+
+def test_host_tensors_reach_no_kernel(monkeypatch):
+    """Tensors on the host are refused before the library hears of them."""
+    def reached(*a):
+        raise AssertionError("reached the library")
+
+    for name in ("_append", "_attend", "_quant"):
+        monkeypatch.setattr(ecfa, name, reached)
+    t = lambda *s, d=torch.bfloat16: torch.zeros(s, dtype=d)  # noqa: E731
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    c, b, r = ecfa.Cache(t(2, 16, 2, 64), t(2, 16, 2, 64)), ecfa.Batch(i32(2, 4), i32(2)), ecfa.Rope(torch.zeros(32, dtype=torch.int64))
+    calls = [lambda: ecfa.ecfa_attend(c, b, t(2, 4, 64)), lambda: ecfa.ecfa_attend(c, b, t(2, 4, 64), out=t(2, 4, 64), workspace=t(1 << 20, d=torch.uint8)),
+             lambda: ecfa.ecfa_append(c, b, t(2, 2, 64), t(2, 2, 64)), lambda: ecfa.ecfa_append(c, b, t(2, 2, 64), t(2, 2, 64), t(2, 4, 64), t(2, 4, 64), r),
+             lambda: ecfa.ecfa_quant(t(2, 256)), lambda: ecfa.ecfa_quant(t(2, 256), 128, t(2, 256, d=torch.uint8), t(2, 2, d=torch.float32))]
+    for call in calls:
+        with pytest.raises(ecf8.Ecf8Error) as e:
+            call()
+        assert e.value.code == ecf8.E_ARG

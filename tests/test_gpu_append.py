@@ -318,3 +318,36 @@ def test_e4m3_is_of_the_quotient_by_the_scale(src):
     ecfa.ecfa_append(ecfa.Cache(pool[0], pool[1], by, by), b, x, -x)
     got = pool.view(2, -1, len(scales), 128)[:, :n].cpu().numpy()
     assert np.array_equal(got[0], want) and np.array_equal(got[1], want ^ 128)
+
+
+def test_refusals_of_tensors_on_the_host_and_of_wrong_shapes(monkeypatch):
+    """Every tensor of a call in turn left on the host, or of a shape or type that does not fit: refused before the library hears of it."""
+    def reached(*a):
+        raise AssertionError("reached the library")
+
+    for name in ("_append", "_attend", "_quant"):
+        monkeypatch.setattr(ecfa, name, reached)
+    t = lambda *s, d=torch.bfloat16, on=DEV: torch.zeros(s, dtype=d, device=on)  # noqa: E731
+    n32 = lambda *s, on=DEV: t(*s, d=torch.int32, on=on)  # noqa: E731
+    f32 = lambda *s, on=DEV: t(*s, d=torch.float32, on=on)  # noqa: E731
+    pool, table, host = t(2, 2, 16, 2, 64), n32(2, 4), torch.device("cpu")
+    rope = lambda on=DEV, pos=None: ecfa.Rope(t(32, d=torch.int64, on=on), pos=pos)  # noqa: E731
+    c, b, k, q = ecfa.Cache(pool[0], pool[1]), ecfa.Batch(table, n32(2)), t(2, 2, 64), t(2, 4, 64)
+    away = ecfa.Batch(table.cpu(), n32(2, on=host))
+    attend = lambda **m: ecfa.ecfa_attend(c, b, **{**dict(q=q, out=q, workspace=t(1 << 20, d=torch.uint8)), **m})  # noqa: E731
+    append = lambda **m: ecfa.ecfa_append(c, b, **{**dict(k=k, v=k, q=q, q_out=q), **m})  # noqa: E731
+    bad = [lambda: ecfa.Cache(pool[0], pool[1].cpu()), lambda: ecfa.Cache(pool[0], pool[1], f32(2, on=host)), lambda: ecfa.Cache(pool[0], pool[1], None, f32(2, on=host)),
+           lambda: ecfa.Batch(table, n32(2, on=host)), lambda: ecfa.Batch(table.cpu(), n32(2)), lambda: ecfa.Batch(table, n32(2), n32(3, on=host), 2), lambda: rope(pos=n32(2, on=host)),
+           lambda: ecfa.ecfa_attend(c, away, q), lambda: ecfa.ecfa_append(c, away, k, k), lambda: ecfa.ecfa_attend(ecfa.Cache(pool[0].cpu(), pool[1].cpu()), b, q),
+           lambda: append(rope=rope(host)), lambda: append(rope=rope(pos=n32(3)))]
+    bad += [lambda m=m: attend(**m) for m in (dict(q=q.cpu()), dict(out=q.cpu()), dict(workspace=t(1 << 20, d=torch.uint8, on=host)), dict(slopes=f32(4, on=host)),
+                                              dict(prefix=n32(2, on=host)), dict(workspace=t(16, d=torch.uint8).expand(1 << 16, 16)), dict(slopes=f32(3)), dict(prefix=n32(3)),
+                                              dict(out=t(2, 2, 64)), dict(q=t(3, 4, 64)), dict(q=t(2, 4, 32)), dict(q=t(2, 256)), dict(q=t(2, 4, 64, d=torch.float16)),
+                                              dict(q=t(2, 64, 4).transpose(1, 2)))]
+    bad += [lambda m=m: append(**m) for m in (dict(k=k.cpu()), dict(v=k.cpu()), dict(q=q.cpu()), dict(q_out=q.cpu()), dict(k=t(2, 4, 64)), dict(q_out=t(2, 2, 64)), dict(q=None))]
+    x, x8, sc = t(4, 256), t(4, 256, d=torch.uint8), f32(4)
+    bad += [lambda: ecfa.ecfa_quant(x.cpu()), lambda: ecfa.ecfa_quant(x, q=x8.cpu()), lambda: ecfa.ecfa_quant(x, scale=sc.cpu()), lambda: ecfa.ecfa_quant(x, 128, x8, sc)]
+    for i, call in enumerate(bad):
+        with pytest.raises(ecf8.Ecf8Error) as e:
+            call()
+        assert e.value.code == ecf8.E_ARG, i
