@@ -32,7 +32,8 @@ extern "C" {
 enum { ECFA_F32 = 1, ECFA_BF16 = 2, ECFA_E4M3 = 3 };
 
 /* Rows of heads: element e of head h of token t is at d[t * token_stride + h * head_stride + e].
- * Strides are in elements; d, and both strides in bytes, are multiples of 16 (ECF8_E_ALIGN). */
+ * Strides are in elements; d, and both strides in bytes, are multiples of 16 (ECF8_E_ALIGN).
+ * Here and below, a stride between things of which there is one does not count. */
 typedef struct ecfa_rows {
     void *d;                       /* DEVICE                                            */
     int64_t token_stride, head_stride;

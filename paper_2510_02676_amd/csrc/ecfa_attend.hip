@@ -229,7 +229,7 @@ int check_attend_rows(const ecfa_rows *r, uint32_t n_tokens)
 {
     if (r->dtype != ECFA_BF16) return ECF8_E_ARG;
     if (n_tokens && !r->d) return ECF8_E_ARG;
-    if (((uintptr_t)r->d & 15) || (r->token_stride * 2 & 15) || (r->head_stride * 2 & 15)) return ECF8_E_ALIGN;
+    if (((uintptr_t)r->d & 15) || (apart(r->token_stride, 2, n_tokens) & 15) || (apart(r->head_stride, 2, r->heads) & 15)) return ECF8_E_ALIGN;
     return ECF8_OK;
 }
 
@@ -278,10 +278,10 @@ int ecfa_attend(const ecfa_cache *cache, const ecfa_batch *batch, const ecfa_att
     }
     a.q = (const uint8_t *)q->d;
     a.out = (uint8_t *)out->d;
-    a.q_tok = q->token_stride * 2;
-    a.q_head = q->head_stride * 2;
-    a.o_tok = out->token_stride * 2;
-    a.o_head = out->head_stride * 2;
+    a.q_tok = apart(q->token_stride, 2, batch->n_tokens);
+    a.q_head = apart(q->head_stride, 2, q->heads);
+    a.o_tok = apart(out->token_stride, 2, batch->n_tokens);
+    a.o_head = apart(out->head_stride, 2, out->heads);
     a.slopes = opts->d_slopes;
     a.prefix = opts->d_prefix_len;
     a.scale_log2 = opts->scale * LOG2E;

@@ -6,6 +6,9 @@ namespace ecfa {
 
 constexpr uint32_t MAX_TOKENS = 1u << 22;      // of a step: a launch counts its threads in 32 bits, 256 to 512 a token
 
+// The bytes from one of n to the next, 0 where there is no next: then the caller's stride does not count, whatever it is.
+inline int64_t apart(int64_t stride, int64_t bytes, uint64_t n) { return n > 1 ? stride * bytes : 0; }
+
 // `used`: whether the call touches the pool (else only head_dim, page_size and dtype count).
 inline int cache_view(const ecfa_cache *c, bool used, CacheView *o)
 {
@@ -16,18 +19,23 @@ inline int cache_view(const ecfa_cache *c, bool used, CacheView *o)
     if (!c->d_k || !c->d_v || c->n_pages == 0 || c->n_pages > 0x7fffffffu || c->kv_heads == 0 || c->kv_heads > (1u << 20)) return ECF8_E_ARG;
     const int64_t e = c->dtype == ECFA_BF16 ? 2 : 1;
     if (((uintptr_t)c->d_k & 15) || ((uintptr_t)c->d_v & 15) || ((uintptr_t)c->d_k_scale & 3) || ((uintptr_t)c->d_v_scale & 3)) return ECF8_E_ALIGN;
-    for (int i = 0; i < 3; i++)
-        if ((c->k_stride[i] * e & 15) || (c->v_stride[i] * e & 15)) return ECF8_E_ALIGN;
+    const uint32_t n[3] = {c->n_pages, c->page_size, c->kv_heads};
+    int64_t k[3], v[3];
+    for (int i = 0; i < 3; i++) {
+        k[i] = apart(c->k_stride[i], e, n[i]);
+        v[i] = apart(c->v_stride[i], e, n[i]);
+        if ((k[i] & 15) || (v[i] & 15)) return ECF8_E_ALIGN;
+    }
     o->k = (uint8_t *)c->d_k;
     o->v = (uint8_t *)c->d_v;
     o->k_scale = c->d_k_scale;
     o->v_scale = c->d_v_scale;
-    o->k_page = c->k_stride[0] * e;
-    o->k_tok = c->k_stride[1] * e;
-    o->k_head = c->k_stride[2] * e;
-    o->v_page = c->v_stride[0] * e;
-    o->v_tok = c->v_stride[1] * e;
-    o->v_head = c->v_stride[2] * e;
+    o->k_page = k[0];
+    o->k_tok = k[1];
+    o->k_head = k[2];
+    o->v_page = v[0];
+    o->v_tok = v[1];
+    o->v_head = v[2];
     o->n_pages = c->n_pages;
     o->near = o->k_tok >= 0 && o->v_tok >= 0 && o->k_tok < (1 << 25) && o->v_tok < (1 << 25);
     return ECF8_OK;

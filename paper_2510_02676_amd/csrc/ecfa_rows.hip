@@ -291,15 +291,15 @@ int check_rows(const ecfa_rows *r, uint32_t n_tokens)
     if (r->dtype != ECFA_F32 && r->dtype != ECFA_BF16) return ECF8_E_ARG;
     if (n_tokens && !r->d) return ECF8_E_ARG;
     const int64_t e = r->dtype == ECFA_F32 ? 4 : 2;
-    if (((uintptr_t)r->d & 15) || (r->token_stride * e & 15) || (r->head_stride * e & 15)) return ECF8_E_ALIGN;
+    if (((uintptr_t)r->d & 15) || (apart(r->token_stride, e, n_tokens) & 15) || (apart(r->head_stride, e, r->heads) & 15)) return ECF8_E_ALIGN;
     return ECF8_OK;
 }
 
-RowsView rows_view(const ecfa_rows *r)
+RowsView rows_view(const ecfa_rows *r, uint32_t n_tokens)
 {
     if (!r) return RowsView{nullptr, 0, 0};
     const int64_t e = r->dtype == ECFA_F32 ? 4 : 2;
-    return RowsView{(uint8_t *)r->d, r->token_stride * e, r->head_stride * e};
+    return RowsView{(uint8_t *)r->d, apart(r->token_stride, e, n_tokens), apart(r->head_stride, e, r->heads)};
 }
 
 template <bool F32, bool F8, bool PAST>
@@ -412,10 +412,10 @@ int ecfa_append(const ecfa_cache *cache, const ecfa_batch *batch, const ecfa_rop
         interleaved = rope->interleaved != 0;
     }
     a.slots = APPEND_THREADS / a.units;
-    a.q = rows_view(q);
-    a.k = rows_view(k);
-    a.v = rows_view(v);
-    a.q_out = rows_view(q_out);
+    a.q = rows_view(q, batch->n_tokens);
+    a.k = rows_view(k, batch->n_tokens);
+    a.v = rows_view(v, batch->n_tokens);
+    a.q_out = rows_view(q_out, batch->n_tokens);
     if (batch->n_tokens == 0) return ECF8_OK;
     const bool f32 = src->dtype == ECFA_F32, f8 = cache->dtype == ECFA_E4M3;
     hipStream_t s = (hipStream_t)stream;
@@ -431,12 +431,12 @@ int ecfa_quant(const void *d_x, uint32_t dtype, uint64_t rows, uint64_t cols, in
     if ((dtype != ECFA_F32 && dtype != ECFA_BF16) || (group != 0 && group != 128) || cols == 0 || cols > (1u << 20) || cols % (group ? 128 : 16)) return ECF8_E_ARG;
     if (rows && (!d_x || !d_q || !d_scale)) return ECF8_E_ARG;
     const int64_t e = dtype == ECFA_F32 ? 4 : 2;
-    if (((uintptr_t)d_x & 15) || (row_stride * e & 15) || ((uintptr_t)d_q & 7) || ((uintptr_t)d_scale & 3)) return ECF8_E_ALIGN;
+    if (((uintptr_t)d_x & 15) || (apart(row_stride, e, rows) & 15) || ((uintptr_t)d_q & 7) || ((uintptr_t)d_scale & 3)) return ECF8_E_ALIGN;
     QuantArgs a{};
     a.x = (const uint8_t *)d_x;
     a.q = d_q;
     a.scale = d_scale;
-    a.row_bytes = row_stride * e;
+    a.row_bytes = apart(row_stride, e, rows);
     a.rows = rows;
     a.cols = (uint32_t)cols;
     a.per_row = (uint32_t)((cols / 8 + 255) / 256);

@@ -132,7 +132,7 @@ class Batch:
     q_start None: seqs).  max_q, max_kv: the most new tokens and keys of a sequence, hints for how the work is split."""
 
     def __init__(self, page_table, kv_len, q_start=None, n_tokens=None, max_q=0, max_kv=0):
-        if page_table.dim() != 2 or page_table.dtype != torch.int32 or page_table.stride(1) != 1:
+        if page_table.dim() != 2 or page_table.dtype != torch.int32 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
             raise _bad("Batch")
         seqs, width = page_table.shape
         if n_tokens is None:

@@ -180,3 +180,12 @@ def test_host_tensors_reach_no_kernel(monkeypatch):
         with pytest.raises(ecf8.Ecf8Error) as e:
             call()
         assert e.value.code == ecf8.E_ARG
+
+
+def test_a_table_of_one_column():
+    table = torch.arange(12, dtype=torch.int32).view(3, 4).t()[:, :1]           # the next column, if there were one, would be 4 on
+    assert table.stride() == (1, 4)
+    b = ecfa.Batch(table, torch.ones(4, dtype=torch.int32))
+    assert b.c.table_stride == 1 and b.c.table_width == 1
+    with pytest.raises(ecf8.Ecf8Error):
+        ecfa.Batch(torch.arange(12, dtype=torch.int32).view(3, 4).t()[:, :2], torch.ones(4, dtype=torch.int32))

@@ -517,3 +517,18 @@ def test_calls_in_flight_on_two_streams():
         torch.cuda.synchronize()
         for i, y in enumerate(got):
             assert torch.equal(y, want[i % 4])
+
+
+def test_strides_that_lead_nowhere():
+    """One token, one head, one page, one token to a page: what the stride to the next would be does not matter."""
+    s = Setting([70], [1], heads=1, kv_heads=1, dim=64, page=1, single=True)
+    want, size = s.want()
+    odd = lambda x, i, by: torch.as_strided(x, x.shape, [by if j == i else n for j, n in enumerate(x.stride())])  # noqa: E731
+    q, out = s.q.to(DEV), torch.zeros((1, 1, 64), dtype=torch.bfloat16, device=DEV)
+    cache = ecfa.Cache(odd(odd(s.k.to(DEV), 1, 7), 2, 3), odd(odd(s.v.to(DEV), 1, 5), 2, 9))
+    got = ecfa.ecfa_attend(cache, s.batch(), odd(odd(q, 0, 5), 1, 3), out=odd(odd(out, 0, 1), 1, 11))
+    assert (np.abs(got.cpu().double().numpy() - want) <= ref.attend_bound(want, size)).all()
+    x = torch.randn((1, 256), device=DEV)
+    for group in (0, 128):
+        a, b = ecfa.ecfa_quant(x, group), ecfa.ecfa_quant(odd(x, 0, 3), group)
+        assert torch.equal(a[0].view(torch.uint8), b[0].view(torch.uint8)) and torch.equal(a[1], b[1])
