@@ -285,8 +285,10 @@ int ecfa_attend(const ecfa_cache *cache, const ecfa_batch *batch, const ecfa_att
     a.slopes = opts->d_slopes;
     a.prefix = opts->d_prefix_len;
     a.scale_log2 = opts->scale * LOG2E;
-    a.cap = opts->softcap;
-    a.cap_inv = opts->softcap > 0 ? 1.f / opts->softcap : 0.f;
+    // A cap above 2^100 changes no score that fp32 tells from its neighbours (below 2^88 by less than 2^-24 of it); below 2^-100 all weights are alike.
+    // So what the kernels work with has a reciprocal and stays finite times log2(e).
+    a.cap = opts->softcap > 0x1p100f ? 0.f : opts->softcap > 0 && opts->softcap < 0x1p-100f ? 0x1p-100f : opts->softcap;
+    a.cap_inv = a.cap > 0 ? 1.f / a.cap : 0.f;
     a.head_dim = cache->head_dim;
     a.heads = q->heads;
     a.kv_heads = cache->kv_heads;

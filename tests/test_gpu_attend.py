@@ -532,3 +532,14 @@ def test_strides_that_lead_nowhere():
     for group in (0, 128):
         a, b = ecfa.ecfa_quant(x, group), ecfa.ecfa_quant(odd(x, 0, 3), group)
         assert torch.equal(a[0].view(torch.uint8), b[0].view(torch.uint8)) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("qn", [1, 4, 50])
+@pytest.mark.parametrize("cap", [1e-45, 1e-40, 2.0 ** -127, 2.0 ** -99, 2.0 ** 99, 2.0 ** 101, 2.0 ** 127, 3.4e38])
+def test_caps_at_the_ends_of_fp32(cap, qn):
+    """Caps without a reciprocal in fp32 make all scores alike; caps that log2(e) times them overflows change none.  A score of 0 stays one."""
+    s = Setting([90, 30], [qn, 1], dim=64)
+    s.q[:, 3] = 0
+    check(s, softcap=cap)
+    s = Setting([90, 30], [qn, 1], dim=64, cache="e4m3")
+    check(s, softcap=cap, scale=3.0)
