@@ -222,6 +222,10 @@ __device__ inline float sum_xor(float x)
     return y + z;
 }
 
+// What a dot product is multiplied by for a score in units of ln 2, kept within the normal numbers of fp32: zero would make NaN of what is masked, an
+// infinity of a dot product of 0.
+__device__ inline float factor_of(const AttendArgs &a, float k_scale) { return __builtin_amdgcn_fmed3f(a.scale_log2 * k_scale, 0x1p-126f, 0x1.fffffep127f); }
+
 // The score of a dot product x, in units of ln 2, with the cap if there is one: softcap * tanh(y), y = scale x / softcap, and
 // tanh(y) = 1 - 2 / (e^(2 y) + 1), which is off by 2^-23 of the cap at most.  That is all for caps up to SIMPLE_CAP (2^-16 of a score); beyond
 // it small y, where that loses digits, take y - y^3 / 3 + 2 y^5 / 15 (error below 2^-26 |y| for |y| < 0.06),

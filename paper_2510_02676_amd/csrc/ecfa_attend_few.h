@@ -53,7 +53,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, uint32_t block, 
     const int32_t *table = a.b.table + (int64_t)s * a.b.table_stride;
     const uint32_t in_page = (1u << a.c.page_shift) - 1;
     const float k_scale = a.c.k_scale ? a.c.k_scale[kvh] : 1.f, v_scale = a.c.v_scale ? a.c.v_scale[kvh] : 1.f;
-    const float to_log2 = a.scale_log2 * k_scale;
+    const float to_log2 = factor_of(a, k_scale);
     const int lds0 = (int)(uint32_t)(uintptr_t)(lds_u8 *)lds + wave * 2 * S::V_BYTES;     // this wave's
     const bool extra = a.cap > 0.f || a.slopes;
     const float cap_in = to_log2 * 2.f * a.cap_inv;

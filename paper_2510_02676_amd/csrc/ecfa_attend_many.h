@@ -97,7 +97,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, uint32_t block,
     const int32_t *table = a.b.table + (int64_t)s * a.b.table_stride;
     const uint32_t in_page = (1u << a.c.page_shift) - 1;
     const float k_scale = a.c.k_scale ? a.c.k_scale[kvh] : 1.f, v_scale = a.c.v_scale ? a.c.v_scale[kvh] : 1.f;
-    const float to_log2 = a.scale_log2 * k_scale, cap_in = to_log2 * 2.f * a.cap_inv;
+    const float to_log2 = factor_of(a, k_scale), cap_in = to_log2 * 2.f * a.cap_inv;
 
     // this lane's row
     const int32_t r = row0 + 32 * wave + col;

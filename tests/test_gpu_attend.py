@@ -543,3 +543,17 @@ def test_caps_at_the_ends_of_fp32(cap, qn):
     check(s, softcap=cap)
     s = Setting([90, 30], [qn, 1], dim=64, cache="e4m3")
     check(s, softcap=cap, scale=3.0)
+
+
+@pytest.mark.parametrize("qn", [1, 4, 50])
+def test_scales_at_the_ends_of_fp32(qn):
+    """Scales so small that the scores vanish, masked keys beside them; the largest scale, with dot products of 0."""
+    for scale in (1e-45, 1e-40):
+        check(Setting([90, 30], [qn, 1], dim=64), scale=scale)
+    s = Setting([90, 30], [qn, 1], dim=64)
+    s.q[:] = 0
+    check(s, scale=3.4e38)
+    s = Setting([90, 30], [qn, 1], dim=64, cache="e4m3")
+    s.k_scale = torch.tensor([1e-45, 2e-45])
+    check(s)
+    check(s, window=20, softcap=3.0)
