@@ -139,6 +139,8 @@ class Batch:
             if q_start is not None:
                 raise _bad("Batch")
             n_tokens = seqs
+        if any(not 0 <= x < 1 << 32 for x in (n_tokens, max_q, max_kv)):
+            raise _bad("Batch")
         self.page_table, self.kv_len, self.q_start = page_table, kv_len, q_start
         self.n_tokens = n_tokens
         self.on = page_table.get_device()
@@ -148,6 +150,8 @@ class Batch:
 
 def rope_freq(rot_dim, base=10000.0, kind=ROPE_PLAIN, factor=1.0, original_len=0.0, beta_fast=32.0, beta_slow=1.0, device="cuda"):
     """(frequencies as int64 bit patterns on the device, scale) of ``ecfa_rope_freq``: what a ``Rope`` takes."""
+    if not 0 < rot_dim < 1 << 32:                                # (as 32 bits it would be another number, of more frequencies than there is room for)
+        raise _bad("ecfa_rope_freq")
     freq, scale = (_u64 * max(1, rot_dim // 2))(), _f32()
     _e._check("ecfa_rope_freq", _lib.ecfa_rope_freq(rot_dim, base, kind, factor, original_len, beta_fast, beta_slow, freq, ctypes.byref(scale)))
     return torch.tensor([int(f) for f in freq], dtype=torch.int64).to(device), float(scale.value)
@@ -199,7 +203,7 @@ def ecfa_attend(cache, batch, q, scale=None, causal=True, window=0, softcap=0.0,
     """Attention of the batch's new tokens over the cache; q and the result (n_tokens, heads, head_dim) BF16.  scale defaults to
     head_dim^-0.5; slopes (heads,) fp32; prefix (seqs,) int32.  Without a workspace one is allocated for the call where it needs it."""
     n, dim, on = batch.n_tokens, cache.head_dim, cache.on
-    if batch.on != on:
+    if batch.on != on or not 0 <= window < 1 << 32:
         raise _bad("ecfa_attend")
     at = _stream_ptr("ecfa_attend", on, stream)
     rq = _rows("ecfa_attend", q, n, 0, dim, on)

@@ -189,3 +189,16 @@ def test_a_table_of_one_column():
     assert b.c.table_stride == 1 and b.c.table_width == 1
     with pytest.raises(ecf8.Ecf8Error):
         ecfa.Batch(torch.arange(12, dtype=torch.int32).view(3, 4).t()[:, :2], torch.ones(4, dtype=torch.int32))
+
+
+def test_counts_that_32_bits_would_change():
+    """ctypes keeps the lower 32 bits of a number and says nothing."""
+    for rot in (0, -2, -64, 3, (1 << 32) + 64):
+        with pytest.raises(ecf8.Ecf8Error) as e:
+            ecfa.rope_freq(rot, device="cpu")
+        assert e.value.code == ecf8.E_ARG
+    table, lens, start = (torch.zeros(s, dtype=torch.int32) for s in ((2, 4), (2,), (3,)))
+    for more in (dict(n_tokens=-1), dict(n_tokens=(1 << 32) + 2), dict(n_tokens=2, max_q=-1), dict(n_tokens=2, max_kv=1 << 32)):
+        with pytest.raises(ecf8.Ecf8Error) as e:
+            ecfa.Batch(table, lens, start, **more)
+        assert e.value.code == ecf8.E_ARG

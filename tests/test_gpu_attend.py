@@ -557,3 +557,13 @@ def test_scales_at_the_ends_of_fp32(qn):
     s.k_scale = torch.tensor([1e-45, 2e-45])
     check(s)
     check(s, window=20, softcap=3.0)
+
+
+def test_windows_that_32_bits_would_change():
+    """-1 would be all keys, 2^32 + 5 five of them."""
+    s = Setting([60], [1], single=True)
+    cache, b, q = s.device_cache(), s.batch(), s.q.to(DEV)
+    for window in (-1, 1 << 32, (1 << 32) + 5):
+        with pytest.raises(ecf8.Ecf8Error) as e:
+            ecfa.ecfa_attend(cache, b, q, window=window)
+        assert e.value.code == ecf8.E_ARG
