@@ -14,7 +14,7 @@ class CompressedAttention:
     """weights: {"q", "k", "v", "o"}: (header, blob on the device, fp32 scale per 128 x 128 weights) each, as ``ecf8_encode(w, lane_syms=64,
     tile_rows=16)`` makes them, of shapes (heads * head_dim, hidden), (kv_heads * head_dim, hidden) twice and (hidden, heads * head_dim).
     cache, batch: ``ecfa.Cache`` and ``ecfa.Batch``, of up to 64 new tokens; rope: ``ecfa.Rope`` or None.  options: scale, window, softcap,
-    slopes, prefix as ``ecfa_attend`` takes them."""
+    slopes, prefix as ``ecfa_attend`` takes them.  What a step would refuse is refused here."""
 
     def __init__(self, weights, heads, cache, batch, rope=None, **options):
         n, dim, kv, dev = batch.n_tokens, cache.head_dim, cache.kv_heads, cache.device
@@ -22,6 +22,9 @@ class CompressedAttention:
         want = {"q": (heads * dim, hidden), "k": (kv * dim, hidden), "v": (kv * dim, hidden), "o": (hidden, heads * dim)}
         if not 1 <= n <= 64 or any((weights[w][0].rows, weights[w][0].cols) != shape for w, shape in want.items()):
             raise ecf8.Ecf8Error("CompressedAttention", ecf8.E_ARG)
+        if any(t is None or t.get_device() != cache.on for w in want for t in weights[w][1:]):
+            raise ecf8.Ecf8Error("CompressedAttention", ecf8.E_ARG)
+        ecfa.check_layer("CompressedAttention", cache, batch, heads, rope, **options)
         self.cache, self.batch, self.rope, self.options, self.out_weight = cache, batch, rope, options, weights["o"]
         empty = lambda shape, dtype: torch.empty(shape, dtype=dtype, device=dev)  # noqa: E731
         self.x8, self.x_scale = empty((n, hidden), torch.uint8), empty((n, hidden // 128), torch.float32)
@@ -32,6 +35,8 @@ class CompressedAttention:
         self.seen8, self.seen_scale = empty((n, heads * dim), torch.uint8), empty((n, heads * dim // 128), torch.float32)
         self.y = empty((n, hidden), torch.float32)
         self.workspace = ecfa.attend_workspace(cache, batch, heads)
+        # the output product as a group of one, whose preparation refuses what the product would: nothing else is done with it
+        ecf8.GemmGroup([{"hdr": weights["o"][0], "blob": weights["o"][1], "x": self.seen8, "w_scale": weights["o"][2], "x_scale": self.seen_scale, "y": self.y}])
 
     def __call__(self, x, stream=None):
         """x (n_tokens, hidden), BF16 or fp32 -> (n_tokens, hidden) fp32, in a buffer that the next call writes again."""

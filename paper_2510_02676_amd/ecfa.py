@@ -123,7 +123,7 @@ class Cache:
         self.on = k.get_device()
         self.c = _Cache(k.data_ptr(), v.data_ptr(), _scale_ptr(k_scale, heads, self.on), _scale_ptr(v_scale, heads, self.on), (_i64 * 3)(*k.stride()[:3]),
                         (_i64 * 3)(*v.stride()[:3]), pages, page, heads, dim, dtype, 0)
-        self.kv_heads, self.head_dim, self.device = heads, dim, k.device
+        self.kv_heads, self.head_dim, self.device, self.scale = heads, dim, k.device, dim ** -0.5 if dim else 1.0
 
 
 class Batch:
@@ -199,11 +199,33 @@ def attend_workspace(cache, batch, heads, stream=None):
     return _empty(n, torch.uint8, cache.device, stream) if n else None
 
 
+def _opts(fn, cache, batch, heads, scale=None, causal=True, window=0, softcap=0.0, slopes=None, prefix=None):
+    """The options of ``ecfa_attend`` as the C structure."""
+    if not 0 <= window < 1 << 32:
+        raise _bad(fn)
+    if slopes is not None and (slopes.dtype != torch.float32 or slopes.shape != (heads,) or not slopes.is_contiguous() or slopes.get_device() != cache.on):
+        raise _bad(fn)
+    return _AttendOpts(cache.scale if scale is None else scale, softcap, None if slopes is None else slopes.data_ptr(),
+                       None if prefix is None else _i32(fn, prefix, batch.kv_len.shape, cache.on), int(causal), window)
+
+
+def check_layer(fn, cache, batch, heads, rope=None, **options):
+    """Raises what ``ecfa_append`` and ``ecfa_attend`` would for these and rows of `heads` query heads, and launches nothing: for programs that build a
+    layer before its first step.  The calls are made for a batch of no tokens."""
+    if batch.on != cache.on or cache.on < 0 or (rope is not None and (rope.on != cache.on or (rope.pos is not None and rope.pos.numel() != batch.n_tokens))):
+        raise _bad(fn)
+    opts = _opts(fn, cache, batch, heads, **options)
+    none = Batch(batch.page_table[:0], batch.kv_len[:0])
+    q, k = (_Rows(None, 0, 0, n, BF16) for n in (heads, cache.kv_heads))
+    _e._check(fn, _append(cache.c, none.c, None if rope is None else rope.c, q, k, k, q, None))
+    _e._check(fn, _attend(cache.c, none.c, opts, q, q, None, 0, None))
+
+
 def ecfa_attend(cache, batch, q, scale=None, causal=True, window=0, softcap=0.0, slopes=None, prefix=None, out=None, workspace=None, stream=None):
     """Attention of the batch's new tokens over the cache; q and the result (n_tokens, heads, head_dim) BF16.  scale defaults to
     head_dim^-0.5; slopes (heads,) fp32; prefix (seqs,) int32.  Without a workspace one is allocated for the call where it needs it."""
     n, dim, on = batch.n_tokens, cache.head_dim, cache.on
-    if batch.on != on or not 0 <= window < 1 << 32:
+    if batch.on != on:
         raise _bad("ecfa_attend")
     at = _stream_ptr("ecfa_attend", on, stream)
     rq = _rows("ecfa_attend", q, n, 0, dim, on)
@@ -211,14 +233,11 @@ def ecfa_attend(cache, batch, q, scale=None, causal=True, window=0, softcap=0.0,
     if out is None:
         out = _empty(q.shape, torch.bfloat16, q.device, stream)
     ro = _rows("ecfa_attend", out, n, heads, dim, on)
-    if slopes is not None and (slopes.dtype != torch.float32 or slopes.shape != (heads,) or not slopes.is_contiguous() or slopes.get_device() != on):
-        raise _bad("ecfa_attend")
+    opts = _opts("ecfa_attend", cache, batch, heads, scale, causal, window, softcap, slopes, prefix)
     if workspace is None:
         workspace = attend_workspace(cache, batch, heads, stream)
     elif workspace.get_device() != on or not workspace.is_contiguous():
         raise _bad("ecfa_attend")
-    opts = _AttendOpts(dim ** -0.5 if scale is None else scale, softcap, None if slopes is None else slopes.data_ptr(),
-                       None if prefix is None else _i32("ecfa_attend", prefix, batch.kv_len.shape, on), int(causal), window)
     rc = _attend(cache.c, batch.c, opts, rq, ro, None if workspace is None else workspace.data_ptr(),
                  0 if workspace is None else workspace.numel(), at)
     if rc:

@@ -115,3 +115,35 @@ def test_shapes_that_do_not_fit():
     with pytest.raises(ecf8.Ecf8Error) as e:
         CompressedAttention(packed, 4, cache, ecfa.Batch(zeros.expand(65, 4).contiguous(), torch.zeros(65, dtype=torch.int32, device=DEV)))
     assert e.value.code == ecf8.E_ARG
+
+
+def test_what_a_step_would_refuse_is_refused_when_it_is_built():
+    packed = {w: weight(r, c, i)[0] for i, (w, r, c) in enumerate((("q", 256, 256), ("k", 128, 256), ("v", 128, 256), ("o", 256, 256)))}
+    pool, before = torch.zeros((2, 4, 16, 2, 64), dtype=torch.bfloat16, device=DEV), torch.zeros((2, 4, 16, 2, 64), dtype=torch.bfloat16, device=DEV)
+    i32 = lambda *s, on=DEV: torch.zeros(s, dtype=torch.int32, device=on)  # noqa: E731
+    cache, batch = ecfa.Cache(pool[0], pool[1]), ecfa.Batch(i32(3, 4), i32(3))
+    make = lambda w=packed, c=cache, b=batch, r=None, **o: CompressedAttention(w, 4, c, b, r, **o)  # noqa: E731
+    fine = [make(), make(r=ecfa.Rope(ecfa.rope_freq(64)[0], pos=i32(3))), make(window=5, softcap=3.0, slopes=torch.zeros(4, device=DEV)), make(prefix=i32(3), scale=0.5, causal=False)]
+    x = torch.zeros((3, 256), dtype=torch.bfloat16, device=DEV)
+    for step in fine:
+        step(x)
+    other = ecf8.ecf8_encode(synth.make_weight(256, 256, 1.7, 0.02, 3).numpy())              # a layout that the products do not read
+    plain = lambda r, c: (lambda b: (b.header, b.to(DEV), torch.ones((-(-r // 128), max(1, c // 128)), device=DEV)))(ecf8.ecf8_encode(synth.make_weight(r, c, 1.7, 0.02, 4).numpy()))  # noqa: E731
+    narrow = ecfa.Cache(*torch.zeros((2, 4, 16, 1, 32), dtype=torch.bfloat16, device=DEV))
+    bad = [lambda: make(window=5, prefix=i32(3)), lambda: make(window=-1), lambda: make(softcap=-1.0), lambda: make(scale=0.0), lambda: make(scale=float("nan")),
+           lambda: make(slopes=torch.zeros(3, device=DEV)), lambda: make(slopes=torch.zeros(4)), lambda: make(prefix=i32(4)), lambda: make(prefix=i32(3, on="cpu")), lambda: make(causal=2),
+           lambda: make(r=ecfa.Rope(ecfa.rope_freq(64)[0], pos=i32(2))), lambda: make(r=ecfa.Rope(ecfa.rope_freq(80)[0])), lambda: make(r=ecfa.Rope(ecfa.rope_freq(64, device="cpu")[0])),
+           lambda: make(r=ecfa.Rope(ecfa.rope_freq(64)[0], scale=float("inf"))), lambda: make(b=ecfa.Batch(i32(3, 4, on="cpu"), i32(3, on="cpu"))),
+           lambda: make({**packed, "o": (other.header, other.to(DEV), packed["o"][2])}), lambda: make({**packed, "o": (packed["o"][0], packed["o"][1].cpu(), packed["o"][2])}),
+           lambda: make({**packed, "o": (*packed["o"][:2], torch.ones((1, 2), device=DEV))}), lambda: make({**packed, "q": (*packed["q"][:2], None)}),
+           lambda: make({**packed, "k": (*packed["k"][:2], packed["k"][2].cpu())}),
+           # 4 heads of 32: 128 columns of the output's weight, where the products take multiples of 256
+           lambda: make({"q": plain(128, 256), "k": plain(32, 256), "v": plain(32, 256), "o": plain(256, 128)}, narrow)]
+    for i, build in enumerate(bad):
+        with pytest.raises(ecf8.Ecf8Error) as e:
+            build()
+        assert e.value.code == ecf8.E_ARG, i
+    with pytest.raises(TypeError):
+        make(windows=5)
+    torch.cuda.synchronize()
+    assert torch.equal(pool, before)                             # zeros were appended, and nothing else
