@@ -351,3 +351,18 @@ def test_refusals_of_tensors_on_the_host_and_of_wrong_shapes(monkeypatch):
         with pytest.raises(ecf8.Ecf8Error) as e:
             call()
         assert e.value.code == ecf8.E_ARG, i
+
+
+def test_bf16_is_of_the_quotient_by_the_scale():
+    """A cache of BF16 with scales: the fp32 quotient, rounded once."""
+    g = torch.Generator().manual_seed(4)
+    scales = torch.tensor([0.0123, 0.3, 7.7, 1.0 / 3.0, 2.0 ** -100, 2.0 ** 100, 1e-30, 1e20])
+    x = torch.randn((300, 8, 64), generator=g) * scales[:, None].clamp(2.0 ** -90, 2.0 ** 90)
+    x[0, :, :4] = torch.tensor([0.0, -0.0, math.inf, -math.inf])
+    pool = torch.zeros((2, 19, 16, 8, 64), dtype=torch.bfloat16, device=DEV)
+    by = scales.to(DEV)
+    b = ecfa.Batch(torch.arange(19, dtype=torch.int32, device=DEV)[None], i32([300]), i32([0, 300]), n_tokens=300)
+    ecfa.ecfa_append(ecfa.Cache(pool[0], pool[1], by, by), b, x.to(DEV), -x.to(DEV))
+    want = (x / scales[:, None]).bfloat16().view(torch.int16)
+    got = pool.view(2, -1, 8, 64)[:, :300].cpu().view(torch.int16)
+    assert torch.equal(got[0], want) and torch.equal(got[1], want ^ -32768)

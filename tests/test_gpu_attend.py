@@ -567,3 +567,14 @@ def test_windows_that_32_bits_would_change():
         with pytest.raises(ecf8.Ecf8Error) as e:
             ecfa.ecfa_attend(cache, b, q, window=window)
         assert e.value.code == ecf8.E_ARG
+
+
+@pytest.mark.parametrize("kv,qn", [([90, 700], [1, 1]), ([90, 700], [50, 3])])
+def test_a_bf16_cache_with_scales(kv, qn):
+    """Scales that are powers of two: bit for bit what keys and values that much larger give."""
+    s = Setting(kv, qn, seed=9)
+    plain, q, k, v = s.device_cache(), s.q.to(DEV), torch.tensor([0.25, 2.0], device=DEV), torch.tensor([4.0, 0.5], device=DEV)
+    larger = ecfa.Cache(plain.k * k[:, None].bfloat16(), plain.v * v[:, None].bfloat16())
+    for more in (dict(), dict(softcap=20.0, window=60)):
+        got = ecfa.ecfa_attend(ecfa.Cache(plain.k, plain.v, k, v), s.batch(), q, **more)
+        assert torch.equal(got, ecfa.ecfa_attend(larger, s.batch(), q, **more))
