@@ -42,20 +42,11 @@ __device__ inline void load8(const uint8_t *p, float *x)
     }
 }
 
-// PAST: written past the caches, for what nobody reads before it would have left them.
-template <bool PAST, class T>
-__device__ inline void put(uint8_t *p, T y)
-{
-    if constexpr (PAST) __builtin_nontemporal_store(y, (T *)p);
-    else *(T *)p = y;
-}
-
-template <bool PAST>
 __device__ inline void store8_bf16(uint8_t *p, const float *x)
 {
     bf16x8 y;
     for (int i = 0; i < 8; i++) y[i] = (__bf16)x[i];          // to nearest even
-    put<PAST>(p, y);
+    *(bf16x8 *)p = y;
 }
 
 // Eight fp32 as E4M3, to nearest even, limited to the largest number of the format; NaN stays NaN.
@@ -93,10 +84,12 @@ __device__ inline void divide16(float *x, float by)
 // halves, 16 u .. interleaved) and walks over the heads of q, k and v, so that its eight sines and cosines are made once.  The angle
 // is position times frequency modulo 2^64 of a turn: the upper 32 bits go to the sine unit, which takes turns, and the
 // error stays below 2^-24 of a turn at any position.
-// Bound by memory: 6472 tokens of BF16 rows with 32 + 2 x 8 heads of 128 elements, 80 MB in and 80 out, take 29.7 us (5.4 TB/s); a single
+// Bound by memory: 6472 tokens of BF16 rows with 32 + 2 x 8 heads of 128 elements, 80 MB in and 80 out, take 35 us (4.6 TB/s); a single
 // token 3.6 us, the time of a launch and of three loads that follow one another (length, page, row).  128 and 512 threads a token: 37.8 and
-// 41.4 us where 256 took 37.4.
-template <bool F32, bool F8, bool INTERLEAVED, bool PAST>
+// 41.4 us where 256 took 37.4.  Results written past the caches make the call alone faster, 27.4 us, but the attention that reads them loses
+// more than that: both together take 221 us this way and 229 past the caches for 16384 tokens in sequences of 512 (E4M3 220.6 and 227.5), 89.0 and 90.6 for 6400 in
+// sequences of 100 (E4M3 86.2 and 90.8), 411 and 413 for a sequence of 6472; only at 65536 tokens in BF16, 800 MB of results, 760 and 748.
+template <bool F32, bool F8, bool INTERLEAVED>
 __global__ __launch_bounds__(APPEND_THREADS) void ecfa_append_kernel(const AppendArgs a)
 {
     const uint32_t t = blockIdx.x;
@@ -150,8 +143,8 @@ __global__ __launch_bounds__(APPEND_THREADS) void ecfa_append_kernel(const Appen
         }
         if (is_q) {
             uint8_t *dst = a.q_out.d + (int64_t)t * a.q_out.tok + (int64_t)hh * a.q_out.head;
-            store8_bf16<PAST>(dst + e0 * 2, x);
-            store8_bf16<PAST>(dst + e1 * 2, x + 8);
+            store8_bf16(dst + e0 * 2, x);
+            store8_bf16(dst + e1 * 2, x + 8);
             continue;
         }
         const uint32_t d0 = is_v ? 16 * u : e0, d1 = is_v ? 16 * u + 8 : e1;
@@ -162,11 +155,11 @@ __global__ __launch_bounds__(APPEND_THREADS) void ecfa_append_kernel(const Appen
             divide16(x, scales[hh]);
         }
         if constexpr (F8) {
-            put<PAST>(dst + d0 * DST, pack8_e4m3(x));
-            put<PAST>(dst + d1 * DST, pack8_e4m3(x + 8));
+            *(u32x2 *)(dst + d0 * DST) = pack8_e4m3(x);
+            *(u32x2 *)(dst + d1 * DST) = pack8_e4m3(x + 8);
         } else {
-            store8_bf16<PAST>(dst + d0 * DST, x);
-            store8_bf16<PAST>(dst + d1 * DST, x + 8);
+            store8_bf16(dst + d0 * DST, x);
+            store8_bf16(dst + d1 * DST, x + 8);
         }
     }
 }
@@ -215,7 +208,7 @@ __device__ inline void store_e4m3(uint8_t *q, const float *x, float inv)
 {
     float y[8];
     for (int i = 0; i < 8; i++) y[i] = x[i] * inv;
-    put<true>(q, pack8_e4m3(y));                               // (past the caches: with what reads it next 11.7 -> 10.3 us at 2048 x 4096)
+    __builtin_nontemporal_store(pack8_e4m3(y), (u32x2 *)q);    // (past the caches: with what reads it next 11.7 -> 10.3 us at 2048 x 4096)
 }
 
 // A scale per row: THREADS threads a row (four rows to a workgroup of 256 if they are 64), the row held in registers between its
@@ -301,23 +294,11 @@ RowsView rows_view(const ecfa_rows *r, uint32_t n_tokens)
     return RowsView{(uint8_t *)r->d, apart(r->token_stride, e, n_tokens), apart(r->head_stride, e, r->heads)};
 }
 
-template <bool F32, bool F8, bool PAST>
+template <bool F32, bool F8>
 void launch_append(const AppendArgs &a, bool interleaved, hipStream_t s)
 {
-    if (interleaved) hipLaunchKernelGGL((ecfa_append_kernel<F32, F8, true, PAST>), dim3(a.b.n_tokens), dim3(APPEND_THREADS), 0, s, a);
-    else hipLaunchKernelGGL((ecfa_append_kernel<F32, F8, false, PAST>), dim3(a.b.n_tokens), dim3(APPEND_THREADS), 0, s, a);
-}
-
-// What is written is read by the attention that follows.  Up to the size of the L2 caches of the eight parts of the card together it is found
-// there (25 MB of a 2048-token chunk: 329 us with its attention, 332 if written past them); more of it is not, and
-// only drives out what else is (80 MB: 29.7 us past them, 37.4 us through them).
-constexpr uint64_t ALL_L2 = 32u << 20;
-
-template <bool F32, bool F8>
-void launch_append_of_size(const AppendArgs &a, uint64_t bytes, bool interleaved, hipStream_t s)
-{
-    if (bytes > ALL_L2) launch_append<F32, F8, true>(a, interleaved, s);
-    else launch_append<F32, F8, false>(a, interleaved, s);
+    if (interleaved) hipLaunchKernelGGL((ecfa_append_kernel<F32, F8, true>), dim3(a.b.n_tokens), dim3(APPEND_THREADS), 0, s, a);
+    else hipLaunchKernelGGL((ecfa_append_kernel<F32, F8, false>), dim3(a.b.n_tokens), dim3(APPEND_THREADS), 0, s, a);
 }
 
 // Threads for a row so that it fits four pieces of eight a thread and rows are spread over the card.  BF16, 4096 rows: 512 columns with 64 threads
@@ -418,9 +399,8 @@ int ecfa_append(const ecfa_cache *cache, const ecfa_batch *batch, const ecfa_rop
     if (batch->n_tokens == 0) return ECF8_OK;
     const bool f32 = src->dtype == ECFA_F32, f8 = cache->dtype == ECFA_E4M3;
     hipStream_t s = (hipStream_t)stream;
-    const uint64_t bytes = (uint64_t)batch->n_tokens * cache->head_dim * (2 * a.q_heads + (f8 ? 2 : 4) * a.kv_heads);
-    if (f32) f8 ? launch_append_of_size<true, true>(a, bytes, interleaved, s) : launch_append_of_size<true, false>(a, bytes, interleaved, s);
-    else f8 ? launch_append_of_size<false, true>(a, bytes, interleaved, s) : launch_append_of_size<false, false>(a, bytes, interleaved, s);
+    if (f32) f8 ? launch_append<true, true>(a, interleaved, s) : launch_append<true, false>(a, interleaved, s);
+    else f8 ? launch_append<false, true>(a, interleaved, s) : launch_append<false, false>(a, interleaved, s);
     return hipGetLastError() == hipSuccess ? ECF8_OK : ECF8_E_HIP;
 }
 
