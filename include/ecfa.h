@@ -64,7 +64,8 @@ typedef struct ecfa_cache {
  * are the last ones), and key j of it is token j % page_size of page
  * page_table[s * table_stride + j / page_size].  A page number outside of the pool is a
  * hole: nothing is written there, and its keys are seen by nobody.  Keys beyond the
- * table's width are holes too. */
+ * table's width are holes too.  Rows before the first start and from the last one on belong
+ * to no sequence: what they would give is not written. */
 typedef struct ecfa_batch {
     const int32_t *d_page_table;   /* DEVICE, n_seqs x table_width                      */
     const int32_t *d_kv_len;       /* DEVICE, n_seqs                                    */
@@ -72,7 +73,7 @@ typedef struct ecfa_batch {
     int64_t table_stride;          /* elements                                          */
     uint32_t table_width;          /* pages; table_width * page_size <= 2^30            */
     uint32_t n_seqs;               /* up to 2^22                                        */
-    uint32_t n_tokens;             /* rows that there are, up to 2^22; starts beyond are cut */
+    uint32_t n_tokens;             /* rows that there are, up to 2^22; starts outside are cut */
     uint32_t max_q;                /* hints for the launch, 0 = not known: the most new tokens and  */
     uint32_t max_kv;               /* the most keys of a sequence.  Results do not depend on them   */
     uint32_t reserved;
@@ -95,7 +96,8 @@ typedef struct ecfa_rope {
 /*
  * ecfa_rope_freq (HOST): fills freq[rot_dim / 2] with base^(-2 j / rot_dim) / (2 pi) turns
  * and *scale (may be NULL) with the factor of ecfa_rope, stretched for contexts longer than
- * a model was trained on:
+ * a model was trained on (RAMP with the steps and the limits of YaRN, arXiv 2309.00071, which
+ * checkpoints that were stretched that way expect):
  *   ECFA_ROPE_PLAIN   as it is; factor and the others are ignored
  *   ECFA_ROPE_LINEAR  all frequencies divided by factor
  *   ECFA_ROPE_BASE    base * factor^(rot_dim / (rot_dim - 2)): the fastest pair stays, the
@@ -130,8 +132,9 @@ int ecfa_append(const ecfa_cache *cache, const ecfa_batch *batch, const ecfa_rop
  *   causal: j <= p, or j < prefix_len[s];   window > 0: j > p - window (not together with prefix_len).
  * A token that sees no key gets zeros.  What is stored in keys and values that a token does
  * not see (NaN, infinities) does not reach it.  q and out are BF16; products of BF16, sums
- * and softmax in fp32; the weights are rounded to BF16 before they meet the values, and
- * their sum is taken of the rounded ones.
+ * and softmax in fp32, so that scores have to lie within fp32; the weights are rounded to BF16
+ * before they meet the values, and their sum is taken of the rounded ones.  With a cap of up to
+ * 64 a score is off by 2^-23 of the cap at most, with a larger one only in proportion to itself.
  *
  * Where there are few rows, long sequences are split among workgroups that leave partial sums in
  * d_workspace (DEVICE, 16-byte aligned, of ecfa_attend_workspace_bytes(), which serves any options

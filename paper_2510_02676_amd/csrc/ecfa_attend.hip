@@ -178,8 +178,9 @@ Shape shape_of(const ecfa_cache *c, const ecfa_batch *b, uint32_t heads, uint32_
     }
     p.many_splits = 1;
     if (p.few) {
-        // As many pieces as make two workgroups on each compute unit, with a step for each wave at least (two for 32 rows); thousands of
-        // sequences need none.  One token of 131072 keys, 64 of up to 8192, 16 times 8 tokens of 4096: two workgroups 108, 49, 77 us; one 131, 52,
+        // As many pieces as make two workgroups on each compute unit, with a step for each wave at least (two for 32 rows), of up to 1024
+        // sequences: every workgroup reads all of their lengths.  One of 32768 keys among 1023 of 32: 327 us, among 1024 (none cut) 435; but 1024 of 512
+        // keys 549 us, 1025 372.  One token of 131072 keys, 64 of up to 8192, 16 times 8 tokens of 4096: two workgroups 108, 49, 77 us; one 131, 52,
         // 88; four 111, 49, 94.  Twice as many steps at least: 2048 keys of one token 12.7 us, 11.4 with one; 8 tokens after 4088 keys 18.8 us,
         // 21.6 with one.
         const uint32_t bytes = p.kc * 32 * (c->dtype == ECFA_E4M3 ? 1 : 2);

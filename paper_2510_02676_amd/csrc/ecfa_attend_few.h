@@ -4,12 +4,14 @@
 // time; its four waves take every fourth step of 32 KU keys each and do not meet until the end, where their (m, l, O) are joined in
 // LDS.  K goes from memory straight into the registers that the matrix cores read it from (lane l: key l % 16, eight elements of
 // the head); V goes from memory into a piece of LDS that belongs to the wave, without touching registers, and is turned when it is read from there.  A step
-// is as many keys as make 16 KB of K and V where registers allow, so that the eight waves of a compute unit have 128 KB on their
-// way: the next step's are fetched as soon as the present one's scores are made.  The 16-byte pieces of a row of V are permuted by
+// is as many keys as make 16 KB of K and V of a wave with 16 rows, so that the eight waves of a compute unit have 128 KB on their
+// way: the next step's are fetched as soon as the present one's scores are made.  Two sub-tiles (NT = 2) do not fit the registers: heads of 65 to 128 in BF16 spill 55 of
+// them to memory (11 up to 96), 26 in E4M3, and of more than 192 133 and 74.  Heads of more than 128 have one workgroup on a compute unit.  The 16-byte pieces of a row of V are permuted by
 // the row's number so that the transposing reads (4 rows and 32 bytes, or 8 rows and 16 bytes, for 16 lanes) do not meet in a bank.
 //
 // Measured, with the kernel that joins the pieces: one token of 131072 keys with 8 key/value heads of 128 in 109 us (537 MB, 4.9 TB/s, of 6.95 that reads
-// reach), 4096 keys 13.4 us; 64 tokens of up to 8192 keys in E4M3 49 us (116 MB of keys and values).
+// reach; 102 where the pool is ordered by head, so that a head's tokens lie together), 4096 keys 13.4 us; 64 tokens of up to 8192 keys in E4M3 49 us (116 MB of keys and
+// values).  32768 keys of heads of 128, 160, 192 and 256: 36, 55, 56 and 70 us (160 runs as 192).
 #pragma once
 #include "ecfa_attend.h"
 

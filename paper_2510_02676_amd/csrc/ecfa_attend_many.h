@@ -6,8 +6,9 @@
 // on the way, once for the four waves.  The 16-byte pieces of a row are permuted by the row's number, so that neither the reads
 // of K (16 rows, one piece) nor the transposing reads of V (4 rows, two pieces) meet in a bank.
 //
-// Measured: 4680 x 4680 tokens of 40 heads of 128 in 482 to 500 us (930 to 900 TFLOP/s, where a large library product reaches 1330); 2048 tokens over
-// 8192 keys, causal, 255 us (944).  The matrix cores are busy for 42 % of the time and the vector ALUs for half of it: a score costs
+// Measured: 4680 x 4680 tokens of 40 heads of 128 in 482 to 536 us (930 to 840 TFLOP/s, where a large library product reaches 1330); 2048 tokens over
+// 8192 keys, causal, 250 to 285 us (960 to 845): unlike cards, the clock under that load.  2048 over 2048 tokens, 32 heads of 128, 160, 192 and 256: 61, 115, 110 and 136 us (160 runs as 192, and
+// heads of more than 128 have one workgroup on a compute unit).  The matrix cores are busy for 42 % of the time and the vector ALUs for half of it: a score costs
 // a multiply-add, an exponential, a share of the maximum, of the sum and of the rounding to BF16 beside its 256 products, and two waves
 // of a SIMD cover one another only in part.
 #pragma once

@@ -331,7 +331,8 @@ int ecfa_rope_freq(uint32_t rot_dim, double base, uint32_t kind, double factor, 
     }
     if (kind == ECFA_ROPE_RAMP && !(original_len > 0 && beta_slow > 0 && beta_fast > beta_slow && std::isfinite(original_len) && std::isfinite(beta_fast)))
         return ECF8_E_ARG;
-    // index at which a pair turns `n` times within original_len: original_len * base^(-2 j / d) / (2 pi) = n
+    // The ramp is that of YaRN (arXiv 2309.00071), with its limits: index at which a pair turns `n` times within original_len,
+    // original_len * base^(-2 j / d) / (2 pi) = n
     const double two_pi = 6.283185307179586476925;
     const auto index_of = [&](double n) { return d * std::log(original_len / (n * two_pi)) / (2 * std::log(base)); };
     double lo = 0, hi = 0;
