@@ -16,7 +16,7 @@ CSRC = os.path.join(PKG, "csrc")
 OBJ_DIR = os.path.join(PKG, "_build")
 SOURCES = ["ecf8_host.cpp", "ecf8_jit.cpp", "ecfw_host.cpp", "ecf8_decode.hip", "ecf8_gemm.hip", "ecf8_gemm_exact.hip",
            "ecf8_encode.hip", "ecfw_decode.hip", "ecfw_encode.hip", "ecfa_rows.hip", "ecfa_attend.hip", "ecfa_attend_bf16.hip",
-           "ecfa_attend_e4m3.hip"]
+           "ecfa_attend_e4m3.hip", "ecfm_gemm.hip", "ecfm_route.hip", "ecfm_rows.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-pthread",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -1,0 +1,116 @@
+// What the kernels of the products of many rows share: their arguments, which rows of which expert a workgroup has, one product of
+// 16 x 128 by 128 x 16 on the FP8 matrix cores.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <cstdint>
+
+#include "ecfm.h"
+
+namespace ecfm {
+
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(8))) int i32x8;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+
+struct ProductArgs {
+    const uint8_t *w, *x;
+    const float *w_scale, *x_scale;
+    const int32_t *starts, *rows;                  // NULL: one expert with every row; row p of X
+    void *y;
+    int64_t w_row, w_expert, x_row, y_row;         // strides: bytes, of Y elements
+    uint32_t n, k, k_blocks, n_blocks;             // rows and columns of W, its 128 x 128 blocks
+    uint32_t m, x_rows, experts, x_per;            // rows of Y and X; x_per: scales a row of X
+    uint32_t n_tiles, first_tile;                  // tiles along n; the first tile along m of this launch
+    uint32_t f32, wide;                            // Y in fp32; four elements of Y may be stored at once
+};
+
+struct Rows {                                      // m0 .. m1 of Y, expert e
+    uint32_t e, m0, m1;
+};
+
+__device__ inline uint32_t cut(int32_t v, uint32_t m) { return v < 0 ? 0 : (uint32_t)v > m ? m : (uint32_t)v; }
+
+// The rows of expert e: begin, and how many.  Starts that fall give none.
+__device__ inline uint32_t rows_of(const ProductArgs &a, uint32_t e, uint32_t *n)
+{
+    const uint32_t b = cut(a.starts[e], a.m), c = cut(a.starts[e + 1], a.m);
+    *n = c > b ? c - b : 0;
+    return b;
+}
+
+// Tile t of BM rows, experts one after the other, each beginning with a tile of its own.  All lanes of a wave together: a lane counts the
+// tiles of ceil(experts / 64) experts, a scan over the lanes finds whose they are.  false: there is no such tile.
+template <uint32_t BM>
+__device__ inline bool find_rows(const ProductArgs &a, uint32_t t, Rows *r)
+{
+    if (!a.starts) {
+        r->e = 0;
+        r->m0 = t * BM;
+        r->m1 = a.m - r->m0 < BM ? a.m : r->m0 + BM;
+        return r->m0 < a.m;
+    }
+    const uint32_t lane = threadIdx.x & 63, per = (a.experts + 63) / 64;
+    uint32_t mine = 0, n;
+    for (uint32_t i = 0; i < per; i++) {
+        const uint32_t e = lane * per + i;
+        if (e < a.experts) {
+            rows_of(a, e, &n);
+            mine += (n + BM - 1) / BM;
+        }
+    }
+    uint32_t upto = mine;
+    for (uint32_t d = 1; d < 64; d *= 2) {
+        const uint32_t v = __shfl_up(upto, d);
+        upto += lane >= d ? v : 0;
+    }
+    const uint64_t hit = __ballot(upto > t);
+    if (!hit) return false;
+    const uint32_t l = (uint32_t)__ffsll((unsigned long long)hit) - 1;
+    uint32_t before = __builtin_amdgcn_readlane(upto - mine, l);
+    for (uint32_t e = l * per; e < a.experts && e < (l + 1) * per; e++) {
+        const uint32_t b = rows_of(a, e, &n), tiles = (n + BM - 1) / BM;
+        if (t - before < tiles) {
+            r->e = e;
+            r->m0 = b + (t - before) * BM;
+            r->m1 = b + n - r->m0 < BM ? b + n : r->m0 + BM;
+            return true;
+        }
+        before += tiles;
+    }
+    return false;
+}
+
+// A lane's 32 of the 128 columns of a row: 16 at 16 g and 16 at 64 + 16 g (g = lane / 16).  Which 32 does not matter as long as both operands
+// take the same; this way a load of a wave covers 64 columns of 16 rows.
+union Piece {
+    i32x8 v;
+    u32x4 h[2];
+};
+
+// d[i] of lane l: row 4 (l / 16) + i of the first operand by row l % 16 of the second, over 128 columns.
+__device__ inline f32x4 product(const Piece &a, const Piece &b)
+{
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a.v, b.v, f32x4{0, 0, 0, 0}, 0, 0, 0, 0, 0, 0);
+}
+
+// Four neighbours along n of row m of Y.
+__device__ inline void store_y(const ProductArgs &a, uint32_t m, uint32_t n, const f32x4 &v)
+{
+    if (n >= a.n) return;
+    const int64_t at = (int64_t)m * a.y_row + n;
+    if (a.wide && n + 4 <= a.n) {
+        if (a.f32) *(f32x4 *)((float *)a.y + at) = v;
+        else *(bf16x4 *)((__bf16 *)a.y + at) = __builtin_convertvector(v, bf16x4);
+        return;
+    }
+    for (uint32_t i = 0; i < 4; i++)
+        if (n + i < a.n) {
+            if (a.f32) ((float *)a.y)[at + i] = v[i];
+            else ((__bf16 *)a.y)[at + i] = (__bf16)v[i];
+        }
+}
+
+} // namespace ecfm
