@@ -41,47 +41,62 @@ __device__ inline uint32_t rows_of(const ProductArgs &a, uint32_t e, uint32_t *n
     return b;
 }
 
-// Tile t of BM rows, experts one after the other, each beginning with a tile of its own.  All lanes of a wave together: a lane counts the
-// tiles of ceil(experts / 64) experts, a scan over the lanes finds whose they are.  false: there is no such tile.
+// The tiles of BM rows, experts one after the other, each beginning with a tile of its own.  All lanes of a wave together: a lane counts the
+// tiles of ceil(experts / 64) experts, a scan over the lanes adds them up; then find() looks for a tile's owner.
 template <uint32_t BM>
-__device__ inline bool find_rows(const ProductArgs &a, uint32_t t, Rows *r)
-{
-    if (!a.starts) {
-        r->e = 0;
-        r->m0 = t * BM;
-        r->m1 = a.m - r->m0 < BM ? a.m : r->m0 + BM;
-        return r->m0 < a.m;
-    }
-    const uint32_t lane = threadIdx.x & 63, per = (a.experts + 63) / 64;
-    uint32_t mine = 0, n;
-    for (uint32_t i = 0; i < per; i++) {
-        const uint32_t e = lane * per + i;
-        if (e < a.experts) {
-            rows_of(a, e, &n);
+struct Tiles {
+    uint32_t mine, upto, all;
+
+    __device__ explicit Tiles(const ProductArgs &a)
+    {
+        if (!a.starts) {
+            all = (a.m + BM - 1) / BM;
+            return;
+        }
+        const uint32_t lane = threadIdx.x & 63, per = (a.experts + 63) / 64;
+        mine = 0;
+        for (uint32_t i = 0; i < per; i++) {
+            const uint32_t e = lane * per + i;
+            uint32_t n = 0;
+            if (e < a.experts) rows_of(a, e, &n);
             mine += (n + BM - 1) / BM;
         }
+        upto = mine;
+        for (uint32_t d = 1; d < 64; d *= 2) {
+            const uint32_t v = __shfl_up(upto, d);
+            upto += lane >= d ? v : 0;
+        }
+        all = __builtin_amdgcn_readlane(upto, 63);
     }
-    uint32_t upto = mine;
-    for (uint32_t d = 1; d < 64; d *= 2) {
-        const uint32_t v = __shfl_up(upto, d);
-        upto += lane >= d ? v : 0;
-    }
-    const uint64_t hit = __ballot(upto > t);
-    if (!hit) return false;
-    const uint32_t l = (uint32_t)__ffsll((unsigned long long)hit) - 1;
-    uint32_t before = __builtin_amdgcn_readlane(upto - mine, l);
-    for (uint32_t e = l * per; e < a.experts && e < (l + 1) * per; e++) {
-        const uint32_t b = rows_of(a, e, &n), tiles = (n + BM - 1) / BM;
-        if (t - before < tiles) {
-            r->e = e;
-            r->m0 = b + (t - before) * BM;
-            r->m1 = b + n - r->m0 < BM ? b + n : r->m0 + BM;
+
+    // false: there is no tile t
+    __device__ bool find(const ProductArgs &a, uint32_t t, Rows *r) const
+    {
+        if (t >= all) return false;
+        if (!a.starts) {
+            r->e = 0;
+            r->m0 = t * BM;
+            r->m1 = a.m - r->m0 < BM ? a.m : r->m0 + BM;
             return true;
         }
-        before += tiles;
+        const uint64_t hit = __ballot(upto > t);
+        if (!hit) return false;
+        const uint32_t per = (a.experts + 63) / 64, l = (uint32_t)__ffsll((unsigned long long)hit) - 1;
+        uint32_t before = __builtin_amdgcn_readlane(upto - mine, l);
+        for (uint32_t e = l * per; e < a.experts && e < (l + 1) * per; e++) {
+            uint32_t n;
+            const uint32_t b = rows_of(a, e, &n), tiles = (n + BM - 1) / BM;
+            if (t - before < tiles) {
+                r->e = e;
+                r->m0 = b + (t - before) * BM;
+                r->m1 = b + n - r->m0 < BM ? b + n : r->m0 + BM;
+                return true;
+            }
+            before += tiles;
+        }
+        return false;
     }
-    return false;
-}
+};
 
 // A lane's 32 of the 128 columns of a row: 16 at 16 g and 16 at 64 + 16 g (g = lane / 16).  Which 32 does not matter as long as both operands
 // take the same; this way a load of a wave covers 64 columns of 16 rows.

@@ -16,7 +16,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void ecfm_few_kernel(const ProductA
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
     const uint32_t n0 = blockIdx.x % a.n_tiles * (16 * NT);
     Rows r;
-    if (!find_rows<16 * MT>(a, a.first_tile + blockIdx.x / a.n_tiles, &r)) return;
+    if (!Tiles<16 * MT>(a).find(a, a.first_tile + blockIdx.x / a.n_tiles, &r)) return;
     const uint8_t *wp[NT], *xp[MT];
     const float *ws[NT], *xs[MT];
     for (int i = 0; i < NT; i++) {
@@ -79,20 +79,143 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void ecfm_few_kernel(const ProductA
     }
 }
 
-// Launches the tiles of `rows` rows of Y, 16 MT (or whatever the kernel takes) at a time.
+typedef __attribute__((address_space(3))) uint8_t lds_u8;
+typedef __attribute__((address_space(3))) const u32x4 lds_u32x4;
+typedef __attribute__((address_space(1))) const uint8_t hbm_u8;
+
+// Many rows: what counts is that the matrix cores are fed.  A workgroup of eight waves has 256 rows of W and BM of X, block after block of 128 columns
+// in one of two buffers in LDS, loaded there without registers while the other one is multiplied.  A row's 16-byte pieces are stored by
+// exclusive or with its number modulo 8, so that the sixteen rows of an operand are read from unlike banks.
+template <uint32_t BM>
+__global__ __launch_bounds__(512, 2) void ecfm_many_kernel(const ProductArgs a)
+{
+    constexpr uint32_t BN = 256, WAVES_N = BM == 256 ? 2 : 4, TN = BN / WAVES_N, TM = BM / (8 / WAVES_N), NI = TN / 16, MJ = TM / 16;
+    constexpr uint32_t BUFFER = (BN + BM) * 128, X_AT = BN * 128, WL = BN / 64, XL = BM / 64;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * BUFFER];
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
+    Rows r;
+    uint32_t n0;
+    {
+        const Tiles<BM> tiles(a);
+        // Workgroups go to the eight dies in turn.  A die gets a run of tiles that lie together, eight along n by some along m, so that its cache serves
+        // rows of W and X to several of them
+        const uint32_t all = tiles.all * a.n_tiles, share = all / 8, more = all % 8, die = blockIdx.x % 8, i = blockIdx.x / 8;
+        if (i >= share + (die < more)) return;
+        const uint32_t id = die * share + (die < more ? die : more) + i;
+        const uint32_t group = id / (8 * tiles.all), first = group * 8, wide = a.n_tiles - first < 8 ? a.n_tiles - first : 8, in = id - group * 8 * tiles.all;
+        n0 = (first + in % wide) * BN;
+        if (!tiles.find(a, in / wide, &r)) return;
+    }
+    const uint32_t wn = wave % WAVES_N, wm = wave / WAVES_N;
+
+    // what this lane loads: piece (lane % 8) ^ (lane / 8) of the rows lane / 8 + 8 * ...
+    const uint32_t piece = 16 * ((lane & 7) ^ (lane >> 3));
+    const uint8_t *wp[WL], *xp[XL];
+    for (uint32_t i = 0; i < WL; i++) {
+        const uint32_t n = n0 + (wave * WL + i) * 8 + (lane >> 3);
+        wp[i] = a.w + (int64_t)r.e * a.w_expert + (int64_t)(n < a.n ? n : a.n - 1) * a.w_row + piece;
+    }
+    for (uint32_t i = 0; i < XL; i++) {
+        const uint32_t m = r.m0 + (wave * XL + i) * 8 + (lane >> 3), p = m < r.m1 ? m : r.m1 - 1;
+        uint32_t x = a.rows ? (uint32_t)a.rows[p] : p;
+        x = x < a.x_rows ? x : 0;
+        xp[i] = a.x + (int64_t)x * a.x_row + piece;
+    }
+    const auto fetch = [&](uint32_t b, uint32_t buffer) {
+        // pieces behind the last column: the block's first one
+        const int64_t at = (int64_t)b * 128 - (b * 128 + piece < a.k ? 0 : piece);
+        uint8_t *dst = lds + buffer * BUFFER;
+#pragma unroll
+        for (uint32_t i = 0; i < WL; i++)
+            __builtin_amdgcn_global_load_lds((hbm_u8 *)(wp[i] + at), (lds_u8 *)(dst + (wave * WL + i) * 1024), 16, 0, 0);
+#pragma unroll
+        for (uint32_t i = 0; i < XL; i++)
+            __builtin_amdgcn_global_load_lds((hbm_u8 *)(xp[i] + at), (lds_u8 *)(dst + X_AT + (wave * XL + i) * 1024), 16, 0, 0);
+    };
+
+    // what this lane multiplies
+    const float *xs[MJ];
+    bool there[MJ];
+    for (uint32_t j = 0; j < MJ; j++) {
+        const uint32_t m = r.m0 + wm * TM + 16 * j + c, p = m < r.m1 ? m : r.m1 - 1;
+        const uint32_t x = a.rows ? (uint32_t)a.rows[p] : p;
+        there[j] = x < a.x_rows;
+        xs[j] = a.x_scale + (uint64_t)(there[j] ? x : 0) * a.x_per;
+    }
+    const uint32_t nb = n0 + wn * TN < a.n ? (n0 + wn * TN) / 128 : a.n_blocks - 1;
+    const float *ws = a.w_scale ? a.w_scale + ((uint64_t)r.e * a.n_blocks + nb) * a.k_blocks : nullptr;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_u8 *)lds, at0 = c * 128 + ((g ^ (c & 7)) << 4);
+    f32x4 sum[NI][MJ] = {};
+    float s[MJ], s_next[MJ];
+    const auto scales = [&](uint32_t b, float *to) {
+        const float w = ws ? ws[b] : 1.f;
+#pragma unroll
+        for (uint32_t j = 0; j < MJ; j++) to[j] = a.x_per > 1 ? w * xs[j][b] : w;
+    };
+
+    fetch(0, 0);
+    scales(0, s_next);
+    uint32_t buffer = 0;
+    for (uint32_t b = 0; b < a.k_blocks; b++, buffer ^= 1) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // loads into LDS are no loads to the barrier's own wait
+        if (b * 128 + 128 > a.k && b * 128 + piece >= a.k)     // columns of X behind the last one count as zeros
+            for (uint32_t i = 0; i < XL; i++) *(u32x4 *)(lds + buffer * BUFFER + X_AT + (wave * XL + i) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+        __syncthreads();                                       // this block is here, and nobody reads the other buffer any more
+#pragma unroll
+        for (uint32_t j = 0; j < MJ; j++) s[j] = s_next[j];
+        if (b + 1 < a.k_blocks) {
+            fetch(b + 1, buffer ^ 1);
+            scales(b + 1, s_next);
+        }
+        const uint32_t w_at = lds0 + buffer * BUFFER + wn * TN * 128 + at0, x_at = lds0 + buffer * BUFFER + X_AT + wm * TM * 128 + at0;
+        const auto read = [&](uint32_t at, uint32_t tile) {
+            Piece p;
+            p.h[0] = *(lds_u32x4 *)(uintptr_t)(at + tile * 2048);
+            p.h[1] = *(lds_u32x4 *)(uintptr_t)((at ^ 64) + tile * 2048);
+            return p;
+        };
+        Piece x[MJ];
+#pragma unroll
+        for (uint32_t j = 0; j < MJ; j++) x[j] = read(x_at, j);
+        Piece w = read(w_at, 0);
+        f32x4 d[MJ];
+#pragma unroll
+        for (uint32_t i = 0; i < NI; i++) {
+            f32x4 now[MJ];
+#pragma unroll
+            for (uint32_t j = 0; j < MJ; j++) now[j] = product(w, x[j]);
+            if (i + 1 < NI) w = read(w_at, i + 1);
+            if (i > 0)
+#pragma unroll
+                for (uint32_t j = 0; j < MJ; j++)
+#pragma unroll
+                    for (int q = 0; q < 4; q++) sum[i - 1][j][q] = fmaf(d[j][q], s[j], sum[i - 1][j][q]);
+#pragma unroll
+            for (uint32_t j = 0; j < MJ; j++) d[j] = now[j];
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < MJ; j++)
+#pragma unroll
+            for (int q = 0; q < 4; q++) sum[NI - 1][j][q] = fmaf(d[j][q], s[j], sum[NI - 1][j][q]);
+    }
+#pragma unroll
+    for (uint32_t j = 0; j < MJ; j++) {
+        const uint32_t m = r.m0 + wm * TM + 16 * j + c;
+        if (m >= r.m1) continue;
+        const float last = a.x_per == 1 ? *xs[j] : 1.f;
+#pragma unroll
+        for (uint32_t i = 0; i < NI; i++) store_y(a, m, n0 + wn * TN + 16 * i + 4 * g, there[j] ? sum[i][j] * last : f32x4{0, 0, 0, 0});
+    }
+}
+
+// Launches a workgroup for each tile of bm x bn that there can be.
 template <class K>
 int launch_tiles(K kernel, ProductArgs a, uint32_t threads, uint32_t bm, uint32_t bn, hipStream_t s)
 {
     a.n_tiles = (a.n + bn - 1) / bn;
     const uint64_t tiles = (uint64_t)(a.m + bm - 1) / bm + (a.starts ? (a.experts < a.m ? a.experts : a.m) : 0);
-    const uint64_t most = 0x7fffffffu / threads / a.n_tiles ? 0x7fffffffu / threads / a.n_tiles : 1;   // of a launch: its threads are counted in 32 bits
-    for (uint64_t t = 0; t < tiles; t += most) {
-        a.first_tile = (uint32_t)t;
-        const uint64_t n = tiles - t < most ? tiles - t : most;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)(n * a.n_tiles)), dim3(threads), 0, s, a);
-        if (hipGetLastError() != hipSuccess) return ECF8_E_HIP;
-    }
-    return ECF8_OK;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((tiles * a.n_tiles + 7) / 8 * 8)), dim3(threads), 0, s, a);
+    return hipGetLastError() == hipSuccess ? ECF8_OK : ECF8_E_HIP;
 }
 
 int check(const ecfm_weights *w, const ecfm_x *x, const ecfm_y *y, ProductArgs *a)
@@ -128,6 +251,9 @@ int check(const ecfm_weights *w, const ecfm_x *x, const ecfm_y *y, ProductArgs *
 
 int launch(const ProductArgs &a, hipStream_t s)
 {
+    const uint32_t each = a.starts ? a.m / a.experts : a.m;
+    if (each > 128) return launch_tiles(ecfm_many_kernel<256>, a, 512, 256, 256, s);
+    if (each > 48) return launch_tiles(ecfm_many_kernel<128>, a, 512, 128, 256, s);
     return launch_tiles(ecfm_few_kernel<1, 1, 2>, a, 64 * FEW_WAVES, 16, 16, s);
 }
 
