@@ -81,17 +81,22 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void ecfm_few_kernel(const ProductA
 
 typedef __attribute__((address_space(3))) uint8_t lds_u8;
 typedef __attribute__((address_space(3))) const u32x4 lds_u32x4;
+typedef __attribute__((address_space(3))) const float lds_f32;
 typedef __attribute__((address_space(1))) const uint8_t hbm_u8;
+
+__device__ const float one = 1.f;
 
 // Many rows: what counts is that the matrix cores are fed.  A workgroup of eight waves has 256 rows of W and BM of X, block after block of 128 columns
 // in one of two buffers in LDS, loaded there without registers while the other one is multiplied.  A row's 16-byte pieces are stored by
-// exclusive or with its number modulo 8, so that the sixteen rows of an operand are read from unlike banks.
+// exclusive or with its number modulo 8, so that the sixteen rows of an operand are read from unlike banks.  Scales come by eight blocks of a row:
+// block by block they would be as many requests to memory as the operands are.
 template <uint32_t BM>
 __global__ __launch_bounds__(512, 2) void ecfm_many_kernel(const ProductArgs a)
 {
     constexpr uint32_t BN = 256, WAVES_N = BM == 256 ? 2 : 4, TN = BN / WAVES_N, TM = BM / (8 / WAVES_N), NI = TN / 16, MJ = TM / 16;
     constexpr uint32_t BUFFER = (BN + BM) * 128, X_AT = BN * 128, WL = BN / 64, XL = BM / 64;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * BUFFER];
+    constexpr uint32_t SCALES_AT = 2 * BUFFER, SCALES = (BM + BN / 128) * 32;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[SCALES_AT + 2 * SCALES];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
     Rows r;
     uint32_t n0;
@@ -108,18 +113,18 @@ __global__ __launch_bounds__(512, 2) void ecfm_many_kernel(const ProductArgs a)
     }
     const uint32_t wn = wave % WAVES_N, wm = wave / WAVES_N;
 
-    // what this lane loads: piece (lane % 8) ^ (lane / 8) of the rows lane / 8 + 8 * ...
+    // what this lane loads: piece (lane % 8) ^ (lane / 8) of the rows lane / 8 + 8 * ..., and their scale of block lane % 8 of eight
     const uint32_t piece = 16 * ((lane & 7) ^ (lane >> 3));
     const uint8_t *wp[WL], *xp[XL];
+    uint32_t x_row[XL];
     for (uint32_t i = 0; i < WL; i++) {
         const uint32_t n = n0 + (wave * WL + i) * 8 + (lane >> 3);
         wp[i] = a.w + (int64_t)r.e * a.w_expert + (int64_t)(n < a.n ? n : a.n - 1) * a.w_row + piece;
     }
     for (uint32_t i = 0; i < XL; i++) {
-        const uint32_t m = r.m0 + (wave * XL + i) * 8 + (lane >> 3), p = m < r.m1 ? m : r.m1 - 1;
-        uint32_t x = a.rows ? (uint32_t)a.rows[p] : p;
-        x = x < a.x_rows ? x : 0;
-        xp[i] = a.x + (int64_t)x * a.x_row + piece;
+        const uint32_t m = r.m0 + (wave * XL + i) * 8 + (lane >> 3), p = m < r.m1 ? m : r.m1 - 1, x = a.rows ? (uint32_t)a.rows[p] : p;
+        x_row[i] = x < a.x_rows ? x : 0;
+        xp[i] = a.x + (int64_t)x_row[i] * a.x_row + piece;
     }
     const auto fetch = [&](uint32_t b, uint32_t buffer) {
         // pieces behind the last column: the block's first one
@@ -132,79 +137,99 @@ __global__ __launch_bounds__(512, 2) void ecfm_many_kernel(const ProductArgs a)
         for (uint32_t i = 0; i < XL; i++)
             __builtin_amdgcn_global_load_lds((hbm_u8 *)(xp[i] + at), (lds_u8 *)(dst + X_AT + (wave * XL + i) * 1024), 16, 0, 0);
     };
-
-    // what this lane multiplies
-    const float *xs[MJ];
-    bool there[MJ];
-    for (uint32_t j = 0; j < MJ; j++) {
-        const uint32_t m = r.m0 + wm * TM + 16 * j + c, p = m < r.m1 ? m : r.m1 - 1;
-        const uint32_t x = a.rows ? (uint32_t)a.rows[p] : p;
-        there[j] = x < a.x_rows;
-        xs[j] = a.x_scale + (uint64_t)(there[j] ? x : 0) * a.x_per;
-    }
-    const uint32_t nb = n0 + wn * TN < a.n ? (n0 + wn * TN) / 128 : a.n_blocks - 1;
-    const float *ws = a.w_scale ? a.w_scale + ((uint64_t)r.e * a.n_blocks + nb) * a.k_blocks : nullptr;
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_u8 *)lds, at0 = c * 128 + ((g ^ (c & 7)) << 4);
-    f32x4 sum[NI][MJ] = {};
-    float s[MJ], s_next[MJ];
-    const auto scales = [&](uint32_t b, float *to) {
-        const float w = ws ? ws[b] : 1.f;
+    // Scales of blocks b .. b + 7 (b a multiple of 8).  Where there are none: a one, again and again
+    const bool x_scaled = a.x_per > 1, w_scaled = a.w_scale != nullptr;
+    const auto fetch_scales = [&](uint32_t b) {
+        const uint32_t at = b + (lane & 7) < a.k_blocks ? b + (lane & 7) : a.k_blocks - 1;
+        uint8_t *dst = lds + SCALES_AT + (b & 8 ? SCALES : 0);
 #pragma unroll
-        for (uint32_t j = 0; j < MJ; j++) to[j] = a.x_per > 1 ? w * xs[j][b] : w;
+        for (uint32_t i = 0; i < XL; i++) {
+            const float *from = x_scaled ? a.x_scale + ((uint64_t)x_row[i] * a.x_per + at) : &one;
+            __builtin_amdgcn_global_load_lds((hbm_u8 *)from, (lds_u8 *)(dst + (wave * XL + i) * 256), 4, 0, 0);
+        }
+        if (wave == 0 && lane < BN / 16) {
+            const uint32_t n = n0 / 128 + (lane >> 3);
+            const float *from = w_scaled ? a.w_scale + (((uint64_t)r.e * a.n_blocks + (n < a.n_blocks ? n : a.n_blocks - 1)) * a.k_blocks + at) : &one;
+            __builtin_amdgcn_global_load_lds((hbm_u8 *)from, (lds_u8 *)(dst + BM * 32), 4, 0, 0);
+        }
     };
 
+    // what this lane multiplies
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_u8 *)lds, at0 = c * 128 + ((g ^ (c & 7)) << 4);
+    const uint32_t xs_at = lds0 + SCALES_AT + (wm * TM + c) * 32, ws_at = lds0 + SCALES_AT + BM * 32 + wn * TN / 128 * 32;
+    f32x4 sum[NI][MJ] = {};
+    // The sum takes a product's block where the products of the next row of tiles are under way: d and s_d are of the row before, across blocks too
+    f32x4 d[MJ] = {};
+    float s[MJ], s_d[MJ] = {};
+
     fetch(0, 0);
-    scales(0, s_next);
+    fetch_scales(0);
     uint32_t buffer = 0;
     for (uint32_t b = 0; b < a.k_blocks; b++, buffer ^= 1) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // loads into LDS are no loads to the barrier's own wait
         if (b * 128 + 128 > a.k && b * 128 + piece >= a.k)     // columns of X behind the last one count as zeros
             for (uint32_t i = 0; i < XL; i++) *(u32x4 *)(lds + buffer * BUFFER + X_AT + (wave * XL + i) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
         __syncthreads();                                       // this block is here, and nobody reads the other buffer any more
-#pragma unroll
-        for (uint32_t j = 0; j < MJ; j++) s[j] = s_next[j];
         if (b + 1 < a.k_blocks) {
             fetch(b + 1, buffer ^ 1);
-            scales(b + 1, s_next);
+            if (b % 8 == 0 && b + 8 < a.k_blocks) fetch_scales(b + 8);
         }
         const uint32_t w_at = lds0 + buffer * BUFFER + wn * TN * 128 + at0, x_at = lds0 + buffer * BUFFER + X_AT + wm * TM * 128 + at0;
+        const uint32_t of_block = (b & 8 ? SCALES : 0) + b % 8 * 4;
         const auto read = [&](uint32_t at, uint32_t tile) {
             Piece p;
             p.h[0] = *(lds_u32x4 *)(uintptr_t)(at + tile * 2048);
             p.h[1] = *(lds_u32x4 *)(uintptr_t)((at ^ 64) + tile * 2048);
             return p;
         };
-        Piece x[MJ];
-#pragma unroll
-        for (uint32_t j = 0; j < MJ; j++) x[j] = read(x_at, j);
-        Piece w = read(w_at, 0);
-        f32x4 d[MJ];
+        Piece x[MJ], w[2];
+        // Reads are issued behind a product, never in front of one that has to wait for earlier ones: the wait would be for them too
+        w[0] = read(w_at, 0);
+        x[0] = read(x_at, 0);
+        x[1] = read(x_at, 1);
 #pragma unroll
         for (uint32_t i = 0; i < NI; i++) {
             f32x4 now[MJ];
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (uint32_t j = 0; j < MJ; j++) now[j] = product(w, x[j]);
-            if (i + 1 < NI) w = read(w_at, i + 1);
-            if (i > 0)
+            for (uint32_t j = 0; j < MJ; j++) {
+                now[j] = product(w[i & 1], x[j]);
+                if (j == 0) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (i == 0) {
 #pragma unroll
-                for (uint32_t j = 0; j < MJ; j++)
+                        for (uint32_t k = 2; k < MJ; k++) x[k] = read(x_at, k);
+                        const float sw = *(lds_f32 *)(uintptr_t)(ws_at + of_block);
 #pragma unroll
-                    for (int q = 0; q < 4; q++) sum[i - 1][j][q] = fmaf(d[j][q], s[j], sum[i - 1][j][q]);
+                        for (uint32_t k = 0; k < MJ; k++) s[k] = sw * *(lds_f32 *)(uintptr_t)(xs_at + k * 512 + of_block);
+                    }
+                    if (i + 1 < NI) w[(i + 1) & 1] = read(w_at, i + 1);
+                }
+                f32x4 &to = i ? sum[i - 1][j] : sum[NI - 1][j];
+                const float by = i ? s[j] : s_d[j];
+#pragma unroll
+                for (int q = 0; q < 4; q++) to[q] = fmaf(d[j][q], by, to[q]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
 #pragma unroll
             for (uint32_t j = 0; j < MJ; j++) d[j] = now[j];
         }
 #pragma unroll
-        for (uint32_t j = 0; j < MJ; j++)
-#pragma unroll
-            for (int q = 0; q < 4; q++) sum[NI - 1][j][q] = fmaf(d[j][q], s[j], sum[NI - 1][j][q]);
+        for (uint32_t j = 0; j < MJ; j++) s_d[j] = s[j];
     }
+#pragma unroll
+    for (uint32_t j = 0; j < MJ; j++)
+#pragma unroll
+        for (int q = 0; q < 4; q++) sum[NI - 1][j][q] = fmaf(d[j][q], s_d[j], sum[NI - 1][j][q]);
 #pragma unroll
     for (uint32_t j = 0; j < MJ; j++) {
         const uint32_t m = r.m0 + wm * TM + 16 * j + c;
         if (m >= r.m1) continue;
-        const float last = a.x_per == 1 ? *xs[j] : 1.f;
+        const uint32_t x = a.rows ? (uint32_t)a.rows[m] : m;
+        const bool there = x < a.x_rows;
+        const float last = a.x_per == 1 && there ? a.x_scale[x] : 1.f;
 #pragma unroll
-        for (uint32_t i = 0; i < NI; i++) store_y(a, m, n0 + wn * TN + 16 * i + 4 * g, there[j] ? sum[i][j] * last : f32x4{0, 0, 0, 0});
+        for (uint32_t i = 0; i < NI; i++) store_y(a, m, n0 + wn * TN + 16 * i + 4 * g, there ? sum[i][j] * last : f32x4{0, 0, 0, 0});
     }
 }
 
