@@ -85,6 +85,7 @@ typedef __attribute__((address_space(3))) const float lds_f32;
 typedef __attribute__((address_space(1))) const uint8_t hbm_u8;
 
 __device__ const float one = 1.f;
+__device__ const u32x4 zeros[1] = {};
 
 // Many rows: what counts is that the matrix cores are fed.  A workgroup of eight waves has 256 rows of W and BM of X, block after block of 128 columns
 // in one of two buffers in LDS, loaded there without registers while the other one is multiplied.  A row's 16-byte pieces are stored by
@@ -126,16 +127,28 @@ __global__ __launch_bounds__(512, 2) void ecfm_many_kernel(const ProductArgs a)
         x_row[i] = x < a.x_rows ? x : 0;
         xp[i] = a.x + (int64_t)x_row[i] * a.x_row + piece;
     }
-    const auto fetch = [&](uint32_t b, uint32_t buffer) {
-        // pieces behind the last column: the block's first one
-        const int64_t at = (int64_t)b * 128 - (b * 128 + piece < a.k ? 0 : piece);
-        uint8_t *dst = lds + buffer * BUFFER;
+    // The i-th of this wave's loads, of the block that the addresses are at
+    const auto fetch = [&](uint32_t buffer, uint32_t i) {
+        uint8_t *dst = lds + buffer * BUFFER + (i < WL ? (wave * WL + i) * 1024 : X_AT + (wave * XL + i - WL) * 1024);
+        __builtin_amdgcn_global_load_lds((hbm_u8 *)(i < WL ? wp[i] : xp[i - WL]), (lds_u8 *)dst, 16, 0, 0);
+    };
+    // Addresses to block b.  In the last one some of the 128 columns may be missing: zeros.  Behind it they stay where they are.
+    const auto advance = [&](uint32_t b) {
+        const uint32_t step = b > 0 && b < a.k_blocks ? 128 : 0;
 #pragma unroll
-        for (uint32_t i = 0; i < WL; i++)
-            __builtin_amdgcn_global_load_lds((hbm_u8 *)(wp[i] + at), (lds_u8 *)(dst + (wave * WL + i) * 1024), 16, 0, 0);
+        for (uint32_t i = 0; i < WL; i++) wp[i] += step;
 #pragma unroll
-        for (uint32_t i = 0; i < XL; i++)
-            __builtin_amdgcn_global_load_lds((hbm_u8 *)(xp[i] + at), (lds_u8 *)(dst + X_AT + (wave * XL + i) * 1024), 16, 0, 0);
+        for (uint32_t i = 0; i < XL; i++) xp[i] += step;
+        if (b * 128 + 128 > a.k && b * 128 + piece >= a.k) {
+#pragma unroll
+            for (uint32_t i = 0; i < WL; i++) wp[i] = (const uint8_t *)zeros;
+#pragma unroll
+            for (uint32_t i = 0; i < XL; i++) xp[i] = (const uint8_t *)zeros;
+        }
+    };
+    const auto arrived = [&] {                                 // the block that is loaded is here for all, and nobody reads the other buffer any more
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // loads into LDS are no loads to the barrier's own wait
+        __syncthreads();
     };
     // Scales of blocks b .. b + 7 (b a multiple of 8).  Where there are none: a one, again and again
     const bool x_scaled = a.x_per > 1, w_scaled = a.w_scale != nullptr;
@@ -160,50 +173,56 @@ __global__ __launch_bounds__(512, 2) void ecfm_many_kernel(const ProductArgs a)
     f32x4 sum[NI][MJ] = {};
     // The sum takes a product's block where the products of the next row of tiles are under way: d and s_d are of the row before, across blocks too
     f32x4 d[MJ] = {};
-    float s[MJ], s_d[MJ] = {};
-
-    fetch(0, 0);
-    fetch_scales(0);
-    uint32_t buffer = 0;
-    for (uint32_t b = 0; b < a.k_blocks; b++, buffer ^= 1) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // loads into LDS are no loads to the barrier's own wait
-        if (b * 128 + 128 > a.k && b * 128 + piece >= a.k)     // columns of X behind the last one count as zeros
-            for (uint32_t i = 0; i < XL; i++) *(u32x4 *)(lds + buffer * BUFFER + X_AT + (wave * XL + i) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
-        __syncthreads();                                       // this block is here, and nobody reads the other buffer any more
-        if (b + 1 < a.k_blocks) {
-            fetch(b + 1, buffer ^ 1);
-            if (b % 8 == 0 && b + 8 < a.k_blocks) fetch_scales(b + 8);
-        }
-        const uint32_t w_at = lds0 + buffer * BUFFER + wn * TN * 128 + at0, x_at = lds0 + buffer * BUFFER + X_AT + wm * TM * 128 + at0;
+    float s[MJ] = {}, s_d[MJ], s_x[MJ], s_w;
+    Piece x[MJ], w[2];
+    const auto read = [&](uint32_t at, uint32_t tile) {
+        Piece p;
+        p.h[0] = *(lds_u32x4 *)(uintptr_t)(at + tile * 2048);
+        p.h[1] = *(lds_u32x4 *)(uintptr_t)((at ^ 64) + tile * 2048);
+        return p;
+    };
+    const auto read_scales = [&](uint32_t b) {
         const uint32_t of_block = (b & 8 ? SCALES : 0) + b % 8 * 4;
-        const auto read = [&](uint32_t at, uint32_t tile) {
-            Piece p;
-            p.h[0] = *(lds_u32x4 *)(uintptr_t)(at + tile * 2048);
-            p.h[1] = *(lds_u32x4 *)(uintptr_t)((at ^ 64) + tile * 2048);
-            return p;
-        };
-        Piece x[MJ], w[2];
-        // Reads are issued behind a product, never in front of one that has to wait for earlier ones: the wait would be for them too
-        w[0] = read(w_at, 0);
-        x[0] = read(x_at, 0);
-        x[1] = read(x_at, 1);
+        s_w = *(lds_f32 *)(uintptr_t)(ws_at + of_block);
+#pragma unroll
+        for (uint32_t j = 0; j < MJ; j++) s_x[j] = *(lds_f32 *)(uintptr_t)(xs_at + j * 512 + of_block);
+    };
+    const uint32_t w_at = lds0 + wn * TN * 128 + at0, x_at = lds0 + X_AT + wm * TM * 128 + at0;
+
+    advance(0);
+#pragma unroll
+    for (uint32_t i = 0; i < WL + XL; i++) fetch(0, i);
+    fetch_scales(0);
+    arrived();
+    w[0] = read(w_at, 0);
+#pragma unroll
+    for (uint32_t j = 0; j < MJ; j++) x[j] = read(x_at, j);
+    read_scales(0);
+    for (uint32_t b = 0; b < a.k_blocks; b++) {
+        const uint32_t here = (b & 1) * BUFFER, there = BUFFER - here;
+        if (b % 8 == 0 && b + 8 < a.k_blocks) fetch_scales(b + 8);
+        advance(b + 1);
+#pragma unroll
+        for (uint32_t j = 0; j < MJ; j++) s_d[j] = s[j], s[j] = s_w * s_x[j];
+        // A row of tiles at a time.  Reads are issued behind a product, never in front of one that has to wait for earlier ones: the wait would be for
+        // them too.  Loads of the next block are issued a few at a time: all at once would hold the products up until the last of them is taken.  Where
+        // the last row's products are left of the block, the barrier: the first reads of the next block then go beside them.
 #pragma unroll
         for (uint32_t i = 0; i < NI; i++) {
             f32x4 now[MJ];
+            if (i == NI - 1) arrived();
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (uint32_t j = 0; j < MJ; j++) {
                 now[j] = product(w[i & 1], x[j]);
-                if (j == 0) {
-                    __builtin_amdgcn_sched_barrier(0);
-                    if (i == 0) {
-#pragma unroll
-                        for (uint32_t k = 2; k < MJ; k++) x[k] = read(x_at, k);
-                        const float sw = *(lds_f32 *)(uintptr_t)(ws_at + of_block);
-#pragma unroll
-                        for (uint32_t k = 0; k < MJ; k++) s[k] = sw * *(lds_f32 *)(uintptr_t)(xs_at + k * 512 + of_block);
-                    }
-                    if (i + 1 < NI) w[(i + 1) & 1] = read(w_at, i + 1);
+                __builtin_amdgcn_sched_barrier(0);
+                if (i + 1 < NI) {
+                    if (j == 0) w[(i + 1) & 1] = read(w_at + here, i + 1);
+                    else if (i * (MJ - 1) + j - 1 < WL + XL) fetch((b & 1) ^ 1, i * (MJ - 1) + j - 1);
+                } else {
+                    if (j == 0) w[0] = read(w_at + there, 0);
+                    x[j] = read(x_at + there, j);
+                    if (j == MJ - 1) read_scales(b + 1);
                 }
                 f32x4 &to = i ? sum[i - 1][j] : sum[NI - 1][j];
                 const float by = i ? s[j] : s_d[j];
@@ -214,22 +233,36 @@ __global__ __launch_bounds__(512, 2) void ecfm_many_kernel(const ProductArgs a)
 #pragma unroll
             for (uint32_t j = 0; j < MJ; j++) d[j] = now[j];
         }
-#pragma unroll
-        for (uint32_t j = 0; j < MJ; j++) s_d[j] = s[j];
     }
 #pragma unroll
     for (uint32_t j = 0; j < MJ; j++)
 #pragma unroll
-        for (int q = 0; q < 4; q++) sum[NI - 1][j][q] = fmaf(d[j][q], s_d[j], sum[NI - 1][j][q]);
+        for (int q = 0; q < 4; q++) sum[NI - 1][j][q] = fmaf(d[j][q], s[j], sum[NI - 1][j][q]);
+    // Y by way of LDS, a piece of 16 rows and TN columns after the other, so that rows are stored 16 bytes a lane and in whole lines: straight from the
+    // registers a store would have 32 bytes of each of 16 rows.  (Nobody reads the buffers any more but for what nobody uses.)
+    uint8_t *const out = lds + wave * 16 * TN * 2;
 #pragma unroll
     for (uint32_t j = 0; j < MJ; j++) {
-        const uint32_t m = r.m0 + wm * TM + 16 * j + c;
-        if (m >= r.m1) continue;
-        const uint32_t x = a.rows ? (uint32_t)a.rows[m] : m;
-        const bool there = x < a.x_rows;
-        const float last = a.x_per == 1 && there ? a.x_scale[x] : 1.f;
+        const uint32_t m = r.m0 + wm * TM + 16 * j, mine = m + c < r.m1 ? m + c : r.m1 - 1, row = a.rows ? (uint32_t)a.rows[mine] : mine;
+        const bool there = row < a.x_rows;
+        const float last = a.x_per == 1 && there ? a.x_scale[row] : 1.f;
+        if (!a.lines) {
+            if (m + c < r.m1)
 #pragma unroll
-        for (uint32_t i = 0; i < NI; i++) store_y(a, m, n0 + wn * TN + 16 * i + 4 * g, there ? sum[i][j] * last : f32x4{0, 0, 0, 0});
+                for (uint32_t i = 0; i < NI; i++) store_y(a, m + c, n0 + wn * TN + 16 * i + 4 * g, there ? sum[i][j] * last : f32x4{0, 0, 0, 0});
+            continue;
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < NI; i++) {
+            const f32x4 v = there ? sum[i][j] * last : f32x4{0, 0, 0, 0};
+            *(bf16x4 *)(out + c * TN * 2 + (((2 * i + g / 2) ^ (c & (TN / 8 - 1))) << 4) + (g & 1) * 8) = __builtin_convertvector(v, bf16x4);
+        }
+#pragma unroll
+        for (uint32_t q = 0; q < TN / 32; q++) {
+            const uint32_t at = q * 64 + lane, to = at / (TN / 8), n = n0 + wn * TN + at % (TN / 8) * 8;
+            const u32x4 v = *(const u32x4 *)(out + to * TN * 2 + (((at % (TN / 8)) ^ (to & (TN / 8 - 1))) << 4));
+            if (m + to < r.m1 && n < a.n) *(u32x4 *)((__bf16 *)a.y + (int64_t)(m + to) * a.y_row + n) = v;
+        }
     }
 }
 
@@ -271,6 +304,7 @@ int check(const ecfm_weights *w, const ecfm_x *x, const ecfm_y *y, ProductArgs *
     a->experts = w->experts;
     a->f32 = y->dtype == ECFA_F32;
     a->wide = a->y_row % 4 == 0 && (uintptr_t)y->d % (4 * e) == 0;
+    a->lines = !a->f32 && a->y_row % 8 == 0 && a->n % 8 == 0 && (uintptr_t)y->d % 16 == 0;
     return ECF8_OK;
 }
 
