@@ -23,7 +23,7 @@ struct ProductArgs {
     int64_t w_row, w_expert, x_row, y_row;         // strides: bytes, of Y elements
     uint32_t n, k, k_blocks, n_blocks;             // rows and columns of W, its 128 x 128 blocks
     uint32_t m, x_rows, experts, x_per;            // rows of Y and X; x_per: scales a row of X
-    uint32_t n_tiles, first_tile;                  // tiles along n; the first tile along m of this launch
+    uint32_t n_tiles;                              // tiles along n
     uint32_t f32, wide, lines;                     // Y in fp32; four elements of Y may be stored at once; BF16, and eight (n a multiple of eight)
 };
 

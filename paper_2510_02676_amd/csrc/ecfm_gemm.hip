@@ -5,6 +5,7 @@ namespace ecfm {
 namespace {
 
 constexpr uint32_t FEW_WAVES = 8;
+constexpr uint64_t MAX_TILES = (1u << 23) - 8;      // of a launch: its threads are counted in 32 bits, 512 a tile
 
 // Few rows: what counts is that W streams from HBM.  A workgroup has 16 NT rows of W and 16 MT rows of X; its eight waves take every
 // eighth block of 128 columns, straight from memory into the matrix cores' operands (a row of W is read by nobody else), and add
@@ -16,7 +17,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void ecfm_few_kernel(const ProductA
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
     const uint32_t n0 = blockIdx.x % a.n_tiles * (16 * NT);
     Rows r;
-    if (!Tiles<16 * MT>(a).find(a, a.first_tile + blockIdx.x / a.n_tiles, &r)) return;
+    if (!Tiles<16 * MT>(a).find(a, blockIdx.x / a.n_tiles, &r)) return;
     const uint8_t *wp[NT], *xp[MT];
     const float *ws[NT], *xs[MT];
     for (int i = 0; i < NT; i++) {
@@ -91,12 +92,13 @@ __device__ const u32x4 zeros[1] = {};
 // in one of two buffers in LDS, loaded there without registers while the other one is multiplied.  A row's 16-byte pieces are stored by
 // exclusive or with its number modulo 8, so that the sixteen rows of an operand are read from unlike banks.  Scales come by eight blocks of a row:
 // block by block they would be as many requests to memory as the operands are.
-template <uint32_t BM>
+template <uint32_t BM, uint32_t BN, uint32_t WAVES_N, uint32_t STAGES>
 __global__ __launch_bounds__(512, 2) void ecfm_many_kernel(const ProductArgs a)
 {
-    constexpr uint32_t BN = 256, WAVES_N = BM == 256 ? 2 : 4, TN = BN / WAVES_N, TM = BM / (8 / WAVES_N), NI = TN / 16, MJ = TM / 16;
+    constexpr uint32_t TN = BN / WAVES_N, TM = BM / (8 / WAVES_N), NI = TN / 16, MJ = TM / 16;
     constexpr uint32_t BUFFER = (BN + BM) * 128, X_AT = BN * 128, WL = BN / 64, XL = BM / 64;
-    constexpr uint32_t SCALES_AT = 2 * BUFFER, SCALES = (BM + BN / 128) * 32;
+    constexpr uint32_t SCALES_AT = STAGES * BUFFER, SCALES = (BM + BN / 128) * 32;
+    static_assert((NI - 1) * MJ >= WL + XL && STAGES >= 2 && STAGES <= 7 && 128 % TN == 0, "");
     __shared__ __attribute__((aligned(1024))) uint8_t lds[SCALES_AT + 2 * SCALES];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
     Rows r;
@@ -129,7 +131,7 @@ __global__ __launch_bounds__(512, 2) void ecfm_many_kernel(const ProductArgs a)
     }
     // The i-th of this wave's loads, of the block that the addresses are at
     const auto fetch = [&](uint32_t buffer, uint32_t i) {
-        uint8_t *dst = lds + buffer * BUFFER + (i < WL ? (wave * WL + i) * 1024 : X_AT + (wave * XL + i - WL) * 1024);
+        uint8_t *dst = lds + buffer + (i < WL ? (wave * WL + i) * 1024 : X_AT + (wave * XL + i - WL) * 1024);
         __builtin_amdgcn_global_load_lds((hbm_u8 *)(i < WL ? wp[i] : xp[i - WL]), (lds_u8 *)dst, 16, 0, 0);
     };
     // Addresses to block b.  In the last one some of the 128 columns may be missing: zeros.  Behind it they stay where they are.
@@ -146,10 +148,9 @@ __global__ __launch_bounds__(512, 2) void ecfm_many_kernel(const ProductArgs a)
             for (uint32_t i = 0; i < XL; i++) xp[i] = (const uint8_t *)zeros;
         }
     };
-    const auto arrived = [&] {                                 // the block that is loaded is here for all, and nobody reads the other buffer any more
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // loads into LDS are no loads to the barrier's own wait
-        __syncthreads();
-    };
+    // The block after the one that is multiplied is here for all, and nobody reads that one any more.  Later ones may be on their way, WL + XL loads a wave
+    // each: loads into LDS are no loads to a barrier's own wait.
+    const auto arrived = [&] { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((STAGES - 2) * (WL + XL)) : "memory"); };
     // Scales of blocks b .. b + 7 (b a multiple of 8).  Where there are none: a one, again and again
     const bool x_scaled = a.x_per > 1, w_scaled = a.w_scale != nullptr;
     const auto fetch_scales = [&](uint32_t b) {
@@ -189,19 +190,23 @@ __global__ __launch_bounds__(512, 2) void ecfm_many_kernel(const ProductArgs a)
     };
     const uint32_t w_at = lds0 + wn * TN * 128 + at0, x_at = lds0 + X_AT + wm * TM * 128 + at0;
 
-    advance(0);
-#pragma unroll
-    for (uint32_t i = 0; i < WL + XL; i++) fetch(0, i);
     fetch_scales(0);
+#pragma unroll
+    for (uint32_t b = 0; b + 1 < STAGES; b++) {
+        advance(b);
+#pragma unroll
+        for (uint32_t i = 0; i < WL + XL; i++) fetch(b * BUFFER, i);
+    }
     arrived();
     w[0] = read(w_at, 0);
 #pragma unroll
     for (uint32_t j = 0; j < MJ; j++) x[j] = read(x_at, j);
     read_scales(0);
+    uint32_t here = 0;
     for (uint32_t b = 0; b < a.k_blocks; b++) {
-        const uint32_t here = (b & 1) * BUFFER, there = BUFFER - here;
+        const uint32_t free = here ? here - BUFFER : (STAGES - 1) * BUFFER, there = here + BUFFER == STAGES * BUFFER ? 0 : here + BUFFER;
         if (b % 8 == 0 && b + 8 < a.k_blocks) fetch_scales(b + 8);
-        advance(b + 1);
+        advance(b + STAGES - 1);
 #pragma unroll
         for (uint32_t j = 0; j < MJ; j++) s_d[j] = s[j], s[j] = s_w * s_x[j];
         // A row of tiles at a time.  Reads are issued behind a product, never in front of one that has to wait for earlier ones: the wait would be for
@@ -218,7 +223,7 @@ __global__ __launch_bounds__(512, 2) void ecfm_many_kernel(const ProductArgs a)
                 __builtin_amdgcn_sched_barrier(0);
                 if (i + 1 < NI) {
                     if (j == 0) w[(i + 1) & 1] = read(w_at + here, i + 1);
-                    else if (i * (MJ - 1) + j - 1 < WL + XL) fetch((b & 1) ^ 1, i * (MJ - 1) + j - 1);
+                    if (i * MJ + j < WL + XL) fetch(free, i * MJ + j);
                 } else {
                     if (j == 0) w[0] = read(w_at + there, 0);
                     x[j] = read(x_at + there, j);
@@ -233,7 +238,9 @@ __global__ __launch_bounds__(512, 2) void ecfm_many_kernel(const ProductArgs a)
 #pragma unroll
             for (uint32_t j = 0; j < MJ; j++) d[j] = now[j];
         }
+        here = there;
     }
+    if (STAGES > 2) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");    // what was loaded behind the last block is here too
 #pragma unroll
     for (uint32_t j = 0; j < MJ; j++)
 #pragma unroll
@@ -272,6 +279,7 @@ int launch_tiles(K kernel, ProductArgs a, uint32_t threads, uint32_t bm, uint32_
 {
     a.n_tiles = (a.n + bn - 1) / bn;
     const uint64_t tiles = (uint64_t)(a.m + bm - 1) / bm + (a.starts ? (a.experts < a.m ? a.experts : a.m) : 0);
+    if (tiles * a.n_tiles > MAX_TILES) return ECF8_E_ARG;
     hipLaunchKernelGGL(kernel, dim3((unsigned)((tiles * a.n_tiles + 7) / 8 * 8)), dim3(threads), 0, s, a);
     return hipGetLastError() == hipSuccess ? ECF8_OK : ECF8_E_HIP;
 }
@@ -308,12 +316,53 @@ int check(const ecfm_weights *w, const ecfm_x *x, const ecfm_y *y, ProductArgs *
     return ECF8_OK;
 }
 
+// What a round of workgroups, one to a compute unit, takes: the same for each tile and that for each block of 128 columns, in us, as measured with the card
+// full (cols 4096 to 14336).  The kernel is the one whose rounds come out shortest.
+struct Shape {
+    uint32_t bm, bn;
+    float tile, block;
+    int (*launch)(const ProductArgs &, hipStream_t);
+};
+
+template <int NT, int MT, int U>
+int few(const ProductArgs &a, hipStream_t s)
+{
+    return launch_tiles(ecfm_few_kernel<NT, MT, U>, a, 64 * FEW_WAVES, 16 * MT, 16 * NT, s);
+}
+
+template <uint32_t BM, uint32_t BN, uint32_t WAVES_N, uint32_t STAGES>
+int many(const ProductArgs &a, hipStream_t s)
+{
+    return launch_tiles(ecfm_many_kernel<BM, BN, WAVES_N, STAGES>, a, 512, BM, BN, s);
+}
+
+const Shape SHAPES[] = {
+    {16, 16, 2.f, 0.10f, few<1, 1, 2>},        {16, 32, 2.f, 0.17f, few<2, 1, 2>},         {16, 64, 2.f, 0.26f, few<4, 1, 1>},
+    {32, 32, 2.f, 0.23f, few<2, 2, 1>},        {32, 64, 2.f, 0.35f, few<4, 2, 1>},         {64, 128, 3.5f, 0.45f, many<64, 128, 2, 6>},
+    {64, 256, 4.f, 0.70f, many<64, 256, 4, 3>}, {128, 128, 4.f, 0.66f, many<128, 128, 2, 4>}, {128, 256, 5.f, 1.05f, many<128, 256, 4, 3>},
+    {256, 256, 6.f, 1.80f, many<256, 256, 2, 2>},
+};
+
 int launch(const ProductArgs &a, hipStream_t s)
 {
-    const uint32_t each = a.starts ? a.m / a.experts : a.m;
-    if (each > 128) return launch_tiles(ecfm_many_kernel<256>, a, 512, 256, 256, s);
-    if (each > 48) return launch_tiles(ecfm_many_kernel<128>, a, 512, 128, 256, s);
-    return launch_tiles(ecfm_few_kernel<1, 1, 2>, a, 64 * FEW_WAVES, 16, 16, s);
+    const Shape *best = nullptr;
+    double least = 0;
+    for (const Shape &v : SHAPES) {
+        // tiles along m: of experts every last one is half empty, and as far as is known here each has rows
+        double tiles = (a.m + v.bm - 1) / v.bm;
+        if (a.starts) {
+            const double hit = a.experts < a.m ? a.experts : a.m, full = (double)a.m / v.bm + 0.5 * hit;
+            tiles = full > hit ? full : hit;
+        }
+        tiles *= (a.n + v.bn - 1) / v.bn;
+        const double rounds = tiles <= 256 ? 1 : a.starts ? tiles / 256 : (double)(((uint64_t)tiles + 255) / 256);
+        const double us = rounds * (v.tile + a.k_blocks * v.block);
+        if (!best || us < least) {
+            best = &v;
+            least = us;
+        }
+    }
+    return best->launch(a, s);
 }
 
 } // namespace
