@@ -98,7 +98,7 @@ int ecfm_gemm_experts(const ecfm_weights *weights, const int32_t *d_starts, cons
  *                     one, lie at d_starts[e] .. d_starts[e + 1]
  *   d_rows            [n_tokens * top]: the token of each sorted pair; -1 behind the last start
  *   d_place           [n_tokens][top]: where a pair is among the sorted ones; -1 where its expert is -1
- * d_workspace: 4-byte aligned, ecfm_route_workspace_bytes() (NULL where that is 0); calls that
+ * d_workspace: 16-byte aligned, ecfm_route_workspace_bytes() (NULL where that is 0); calls that
  * overlap in time need one each.  The same call gives the same bits.
  * ECF8_E_ARG: experts 0 or over 1024, top 0 or over 32 or more than the groups chosen hold, groups that do
  * not divide experts or over 64, top_groups 0 or over groups, n_tokens over 2^22, scale not finite.
