@@ -264,12 +264,10 @@ __global__ __launch_bounds__(THREADS) void ecfm_choose_kernel(const RouteArgs a)
         double got = 0, total = 0;
         for (uint32_t j = 0; j < a.top; j++) {
             uint64_t k = key[0];
-            double v = score[0];
             uint32_t e = lane;
             for (int q = 1; q < PER; q++)
                 if (key[q] > k) {
                     k = key[q];
-                    v = score[q];
                     e = lane + 64 * q;
                 }
             const uint32_t hi = (uint32_t)(k >> 32), hi_most = wave_most(hi);
@@ -284,14 +282,17 @@ __global__ __launch_bounds__(THREADS) void ecfm_choose_kernel(const RouteArgs a)
                 }
             }
             const uint32_t at_lane = (uint32_t)__ffsll((unsigned long long)who) - 1, at = (uint32_t)__builtin_amdgcn_readlane((int)e, at_lane);
-            const double w = of_lane(v, at_lane);
+            double w = 0;
+            for (int q = 0; q < PER; q++)
+                if (at / 64 == (uint32_t)q) {                  // (the same for all lanes)
+                    w = of_lane(score[q], at_lane);
+                    key[q] = lane == at_lane ? 0 : key[q];
+                }
             total += w;
             if (lane == j) {
                 id = (int32_t)at;
                 got = w;
             }
-            for (int q = 0; q < PER; q++)
-                if (lane + 64 * q == at) key[q] = 0;
         }
         if (a.normalise) got = total > 0 ? got / total : 0;
         if (lane < a.top) {
