@@ -147,18 +147,18 @@ struct CombineArgs {
     By by_row;
 };
 
-// Eight elements as they come from memory.
+// Eight elements as they come from memory, past the caches: nobody reads them again (4096 tokens of 8 x 7168: 116 us through them, 106 so).
 template <bool F32>
 struct Eight {
     f32x4 a, b;
-    __device__ void load(const uint8_t *p) { a = *(const f32x4 *)p, b = *(const f32x4 *)(p + 16); }
+    __device__ void load(const uint8_t *p) { a = __builtin_nontemporal_load((const f32x4 *)p), b = __builtin_nontemporal_load((const f32x4 *)(p + 16)); }
     __device__ float at(int i) const { return i < 4 ? a[i] : b[i - 4]; }
 };
 
 template <>
 struct Eight<false> {
     ecfa::bf16x8 a;
-    __device__ void load(const uint8_t *p) { a = *(const ecfa::bf16x8 *)p; }
+    __device__ void load(const uint8_t *p) { a = __builtin_nontemporal_load((const ecfa::bf16x8 *)p); }
     __device__ float at(int i) const { return (float)a[i]; }
 };
 
