@@ -30,7 +30,7 @@ extern "C" {
 /* The weights of one product, or of `experts` of the same shape: row n of expert e is the cols bytes at
  * d + e * expert_stride + n * row_stride; the scale of its columns 128 b .. 128 b + 127 is
  * d_scale[(e * ceil(rows / 128) + n / 128) * ceil(cols / 128) + b] (NULL: ones).
- * d and both strides are multiples of 16 (ECF8_E_ALIGN). */
+ * d and both strides are multiples of 16 (ECF8_E_ALIGN); row_stride is 0 .. 2^24 (ECF8_E_ARG). */
 typedef struct ecfm_weights {
     const uint8_t *d;              /* DEVICE                                            */
     const float *d_scale;          /* DEVICE or NULL                                    */
@@ -44,7 +44,7 @@ typedef struct ecfm_weights {
 /* X: row r is the cols bytes (cols of the weights) at d + r * row_stride; its scale is d_scale[r]
  * (scale_cols = 1), or d_scale[r * scale_cols + b] for its columns 128 b .. 128 b + 127 (scale_cols =
  * ceil(cols / 128)), or one (NULL, scale_cols = 0).  Where there is one block of 128, both are the same.
- * d and row_stride are multiples of 16. */
+ * d and row_stride are multiples of 16; row_stride is 0 .. 2^32 - 16. */
 typedef struct ecfm_x {
     const uint8_t *d;              /* DEVICE                                            */
     const float *d_scale;          /* DEVICE or NULL                                    */
@@ -67,7 +67,7 @@ typedef struct ecfm_y {
  * for the x->rows = y->rows rows; weights->experts is 1.  The FP8 matrix cores sum a block, and drop what lies
  * more than 13 bits below the largest of 8 neighbouring products: a result can be off by up to 7 * 2^-13 of the sum of the
  * products' magnitudes (2^-16 of its size on ordinary data).  Blocks are joined in fp32, with the product of the two
- * scales rounded to fp32 (a row's single scale multiplies the finished sum); then one rounding to BF16.  NaN stay
+ * scales rounded to fp32; then one rounding to BF16.  NaN stay
  * in the rows and columns of Y whose X or W hold them.
  */
 int ecfm_gemm(const ecfm_weights *weights, const ecfm_x *x, const ecfm_y *y, void *stream);
@@ -77,6 +77,7 @@ int ecfm_gemm(const ecfm_weights *weights, const ecfm_x *x, const ecfm_y *y, voi
  * weights with row d_rows[p] of X (row p where d_rows is NULL; x->rows = y->rows then).  d_starts: DEVICE,
  * experts + 1, rising; values outside of 0 .. y->rows are cut.  Rows of Y before the first start and from the last one on
  * are left as they were.  A row number outside of X gives a row of zeros.
+ * ECF8_E_ARG also, here and above: over 2^23 - 8 tiles of 256 x 256 results.
  */
 int ecfm_gemm_experts(const ecfm_weights *weights, const int32_t *d_starts, const ecfm_x *x, const int32_t *d_rows,
                       const ecfm_y *y, void *stream);

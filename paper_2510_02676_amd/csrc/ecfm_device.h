@@ -23,7 +23,7 @@ struct ProductArgs {
     int64_t w_row, w_expert, x_row, y_row;         // strides: bytes, of Y elements
     uint32_t n, k, k_blocks, n_blocks;             // rows and columns of W, its 128 x 128 blocks
     uint32_t m, x_rows, experts, x_per;            // rows of Y and X; x_per: scales a row of X
-    uint32_t n_tiles;                              // tiles along n
+    uint32_t n_tiles, m_tiles;                     // tiles along n; along m at most
     uint32_t f32, wide, lines;                     // Y in fp32; four elements of Y may be stored at once; BF16, and eight (n a multiple of eight)
 };
 
@@ -50,7 +50,7 @@ struct Tiles {
     __device__ explicit Tiles(const ProductArgs &a)
     {
         if (!a.starts) {
-            all = (a.m + BM - 1) / BM;
+            all = a.m_tiles;
             return;
         }
         const uint32_t lane = threadIdx.x & 63, per = (a.experts + 63) / 64;
@@ -67,6 +67,7 @@ struct Tiles {
             upto += lane >= d ? v : 0;
         }
         all = __builtin_amdgcn_readlane(upto, 63);
+        all = all < a.m_tiles ? all : a.m_tiles;               // (starts that fall could claim more)
     }
 
     // false: there is no tile t

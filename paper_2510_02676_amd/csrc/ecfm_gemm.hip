@@ -353,13 +353,17 @@ __global__ __launch_bounds__(512, 2) void ecfm_many_kernel(const ProductArgs a)
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // what was loaded behind the last block is here too
 }
 
-// Launches a workgroup for each tile of bm x bn that there can be, or `most` that take them in turn.
+// The most tiles along m that there can be, and of bm x bn.
+uint32_t tiles_of(const ProductArgs &a, uint32_t bm) { return (a.m + bm - 1) / bm + (a.starts ? (a.experts < a.m ? a.experts : a.m) : 0); }
+uint64_t tiles_of(const ProductArgs &a, uint32_t bm, uint32_t bn) { return (uint64_t)tiles_of(a, bm) * ((a.n + bn - 1) / bn); }
+
+// Launches a workgroup for each of them, or `most` that take them in turn.
 template <class K>
 int launch_tiles(K kernel, ProductArgs a, uint32_t threads, uint32_t bm, uint32_t bn, uint32_t most, hipStream_t s)
 {
     a.n_tiles = (a.n + bn - 1) / bn;
-    const uint64_t tiles = ((uint64_t)(a.m + bm - 1) / bm + (a.starts ? (a.experts < a.m ? a.experts : a.m) : 0)) * a.n_tiles;
-    if (tiles > MAX_TILES) return ECF8_E_ARG;
+    a.m_tiles = tiles_of(a, bm);
+    const uint64_t tiles = tiles_of(a, bm, bn);
     hipLaunchKernelGGL(kernel, dim3((unsigned)(((tiles < most ? tiles : most) + 7) / 8 * 8)), dim3(threads), 0, s, a);
     return hipGetLastError() == hipSuccess ? ECF8_OK : ECF8_E_HIP;
 }
@@ -432,6 +436,7 @@ int launch(const ProductArgs &a, hipStream_t s)
     const Shape *best = nullptr;
     double least = 0;
     for (const Shape &v : SHAPES) {
+        if (tiles_of(a, v.bm, v.bn) > MAX_TILES) continue;
         // tiles along m: of experts every last one is half empty, and as far as is known here each has rows
         double tiles = (a.m + v.bm - 1) / v.bm;
         if (a.starts) {
@@ -447,7 +452,7 @@ int launch(const ProductArgs &a, hipStream_t s)
             least = us;
         }
     }
-    return best->launch(a, s);
+    return best ? best->launch(a, s) : ECF8_E_ARG;
 }
 
 } // namespace

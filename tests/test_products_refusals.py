@@ -37,7 +37,8 @@ def experts(w=None, starts=AT, xx=None, rows=None, yy=None):
 
 
 @pytest.mark.parametrize("more,code", [(dict(d=None), A), (dict(rows=0), A), (dict(rows=(1 << 24) + 1), A), (dict(cols=0), A), (dict(cols=40), A), (dict(cols=(1 << 24) + 16), A),
-                                       (dict(experts=0), A), (dict(experts=4097), A), (dict(d=AT + 8), E), (dict(row_stride=264), E), (dict(d_scale=AT + 2), E)])
+                                       (dict(experts=0), A), (dict(experts=4097), A), (dict(d=AT + 8), E), (dict(row_stride=264), E), (dict(d_scale=AT + 2), E),
+                                       (dict(row_stride=-256), A), (dict(row_stride=(1 << 24) + 16), A)])
 def test_weights(more, code):
     assert gemm(w=weights(**more)) == code
     assert experts(w=weights(**dict(dict(experts=3), **more))) == code
@@ -45,7 +46,8 @@ def test_weights(more, code):
 
 
 @pytest.mark.parametrize("more,code", [(dict(d=None), A), (dict(d_scale=None), A), (dict(scale_cols=0), A), (dict(scale_cols=3), A), (dict(rows=4), A), (dict(rows=(1 << 28) + 1), A),
-                                       (dict(d=AT + 4), E), (dict(row_stride=250), E), (dict(d_scale=AT + 1), E)])
+                                       (dict(d=AT + 4), E), (dict(row_stride=250), E), (dict(d_scale=AT + 1), E),
+                                       (dict(row_stride=-256), A), (dict(row_stride=1 << 32), A)])
 def test_x(more, code):
     assert gemm(xx=x(**more)) == code
     assert experts(xx=x(**more)) == code
