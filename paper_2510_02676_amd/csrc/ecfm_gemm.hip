@@ -9,7 +9,8 @@ constexpr uint64_t MAX_TILES = (1u << 23) - 8;      // of a launch: its threads 
 
 // Few rows: what counts is that W streams from HBM.  A workgroup has 16 NT rows of W and 16 MT rows of X; its eight waves take every
 // eighth block of 128 columns, straight from memory into the matrix cores' operands (a row of W is read by nobody else), and add
-// up through LDS, in the order of the waves.
+// up through LDS, in the order of the waves.  Columns are split within a workgroup, so that nothing has to be joined elsewhere.  16 x 14336 x 4096: 12.2 us,
+// 4.9 TB/s of W, with the start of the waves and the sum at the end; W alone would take 8.5.
 template <int NT, int MT, int U>
 __global__ __launch_bounds__(64 * FEW_WAVES) void ecfm_few_kernel(const ProductArgs a)
 {
@@ -90,7 +91,10 @@ __device__ const u32x4 zeros[1] = {};
 // Many rows: what counts is that the matrix cores are fed.  A workgroup of eight waves has tiles of BN rows of W by BM of X, one after the other; block after
 // block of 128 columns goes through a ring of STAGES buffers in LDS, loaded there without registers while an earlier one is multiplied, across
 // the tiles' borders too.  A row's 16-byte pieces are stored by exclusive or with its number modulo 8, so that the sixteen rows of an operand
-// are read from unlike banks.  Scales come by eight blocks of a row: block by block they would be as many requests to memory as the operands are.
+// are read from unlike banks.  Scales come by eight blocks of a row: block by block they would be as many requests to memory as the operands are
+// (8192 x 14336 x 4096: 531 us, 466 so).
+// 256 x 256: 2.36 PFLOP/s at 8192 x 14336 x 4096, matrix cores 59 % of the time busy at 1.85 GHz, where the power holds the card (fewer cycles did
+// not take less time).  128 x 256, 4096 tokens: 6.4 TB/s of W, which is read once for each 128 rows of an expert.  64 x 256, 48 tokens: 6.07 TB/s.
 template <uint32_t BM, uint32_t BN, uint32_t WAVES_N, uint32_t STAGES>
 __global__ __launch_bounds__(512, 2) void ecfm_many_kernel(const ProductArgs a)
 {
@@ -402,7 +406,16 @@ int check(const ecfm_weights *w, const ecfm_x *x, const ecfm_y *y, ProductArgs *
 }
 
 // What a round of workgroups, one to a compute unit, takes: the same for each tile and that for each block of 128 columns, in us, as measured with the card
-// full (cols 2048 to 14336).  The kernel is the one whose rounds come out shortest.
+// full (cols 2048 to 14336).  The kernel is the one whose rounds come out shortest.  In us, that kernel and its neighbours, inputs past the caches:
+//   16 x 14336 x 4096                  16 x 64 15.1, 16 x 32 17.9, 64 x 128 19.1
+//   64 x 4096 x 4096                   32 x 32 12.2, 16 x 64 13.1, 64 x 128 18.6
+//   777 x 1001 x 2064                  32 x 64 12.0, 32 x 32 13.7, 64 x 128 14.2
+//   200 x 4096 x 4096                  64 x 128 18.3, 128 x 128 21.2, 32 x 64 28.5
+//   2048 x 4096 x 4096                 128 x 256 38, 128 x 128 46, 256 x 256 62
+//   8192 x 14336 x 4096                256 x 256 411, 128 x 256 479, 128 x 128 601
+//   1 token of 8 experts, 4096 x 7168  64 x 128 44.2, 16 x 64 42.8, 64 x 256 53.5
+//   48 tokens, 256 of 7168 x 2048      64 x 256 417, 16 x 64 439, 128 x 128 419
+//   4096 tokens, 256 of 4096 x 7168    128 x 256 1788, 128 x 128 1975, 256 x 256 2179
 struct Shape {
     uint32_t bm, bn;
     float tile, block;

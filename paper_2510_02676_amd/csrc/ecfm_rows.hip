@@ -35,7 +35,7 @@ struct GateArgs {
 // silu(g) * u of eight: with t = exp(-|g|), g / (1 + t), or g t / (1 + t) below zero, so that nothing overflows on the way; at -infinity g t would be
 // NaN.  t = 2^e (1 + r ln 2), e the product of -|g| and log2(e) in fp32 and r what that leaves out, is within two of its last places (0 where
 // it is below fp32's normal numbers).  exp, a division and clamps were 373 instructions for the eight and as long as their bytes (86 us at 32768 x 2048;
-// 72 with a reciprocal).
+// 72 with a reciprocal, 58 so: 5.8 TB/s).
 template <bool F32>
 __device__ inline void gated8(const uint8_t *g, const uint8_t *u, float *h)
 {
