@@ -40,7 +40,8 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void ecfm_few_kernel(const ProductA
     for (uint32_t first = wave; first < a.k_blocks; first += U * FEW_WAVES) {
         Piece w[U][NT], x[U][MT];
         float sw[U][NT], sx[U][MT];
-        // blocks behind the last one: the last one again, times nothing (its own product is part of the sum, so a NaN is in it anyway)
+        // blocks behind the last one: the last one again, with scales of 0, both, since infinity times 0 is none (its own product is part of the sum, so a
+        // NaN is in it anyway)
         for (int u = 0; u < U; u++) {
             const uint32_t b = first + u * FEW_WAVES, at = b < a.k_blocks ? b : a.k_blocks - 1;
             // in the last block some of the 128 columns may be missing: those of X count as zeros, in those of W's place stands the row's beginning
@@ -55,7 +56,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void ecfm_few_kernel(const ProductA
                 x[u][j].h[1] = *(const u32x4 *)(xp[j] + far);
                 if (at * 128 + 16 * g >= a.k) x[u][j].h[0] = u32x4{0, 0, 0, 0};
                 if (at * 128 + 64 + 16 * g >= a.k) x[u][j].h[1] = u32x4{0, 0, 0, 0};
-                sx[u][j] = a.x_per ? xs[j][a.x_per > 1 ? at : 0] : 1.f;
+                sx[u][j] = b >= a.k_blocks ? 0.f : a.x_per ? xs[j][a.x_per > 1 ? at : 0] : 1.f;
             }
         }
         for (int u = 0; u < U; u++)

@@ -125,6 +125,24 @@ def test_scales_of_any_size_and_sign():
     assert not got[7].isfinite().any() and got[:7].isfinite().all() and got[8:].isfinite().all()
 
 
+@pytest.mark.parametrize("m,n,k", [(9, 40, 272), (40, 100, 1152), (70, 140, 128), (300, 290, 400)])
+def test_infinite_scales(m, n, k):
+    """A block whose scale is infinite gives an infinity of its sum's sign, whichever block of the row it is."""
+    x, xs, w, ws = inputs(m, n, k, "group", seed=10)
+    for b in range(ref.blocks(k)):
+        xs[b % m, b] = float("inf")
+        ws[0, b] *= -1 if b % 2 else 1
+    xs[m - 1, -1] = float("-inf")
+    got = ecfm.ecfm_gemm(ecfm.Weights(dev(w), dev(ws)), dev(x), dev(xs), dtype=torch.float32).cpu().numpy()
+    for r, b in [(b % m, b) for b in range(ref.blocks(k))] + [(m - 1, ref.blocks(k) - 1)]:
+        if np.isinf(arr(xs)[r]).sum() > 1:
+            continue
+        part = ref.E4M3[arr(x)[r, 128 * b:128 * b + 128]] @ ref.E4M3[arr(w)[:, 128 * b:128 * b + 128]].T
+        clear = np.abs(part) > 2.0 ** -9 * np.abs(ref.E4M3[arr(x)[r, 128 * b:128 * b + 128]]).sum() * 448
+        want = np.sign(part) * np.sign(arr(ws)[np.arange(n) // 128, b]) * np.float64(arr(xs)[r, b])
+        assert clear.any() and (got[r][clear] == want[clear]).all()
+
+
 @pytest.mark.parametrize("m", [3, 70, 200])
 def test_operands_further_apart_than_32_bits(m):
     n, k, far = 40, 144, (1 << 31) // m // 16 * 16 + 16 * 1000             # rows of X; the last one lies beyond 2^31, in Y beyond 2^32 bytes
