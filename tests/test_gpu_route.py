@@ -132,3 +132,42 @@ def test_a_captured_call_and_the_same_routes_again():
             starts, rows, place = ref.sort_pairs(ids, 64)
             assert routes.ids.tolist() == ids and routes.starts.tolist() == starts and routes.rows.tolist() == rows and routes.place.tolist() == place
             check(new, 6, routes=routes)
+
+
+@pytest.mark.parametrize("tokens,experts,top", [(32, 256, 8), (33, 256, 8), (17, 512, 4), (512, 96, 5), (513, 96, 5), (2049, 257, 3), (4097, 1000, 3), (9001, 1024, 2), (20011, 1000, 3), (40001, 64, 2),
+                                                (65535, 9, 2), (65536, 9, 2)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_shares_of_the_workgroups(tokens, experts, top, dtype):
+    test_many_tokens(tokens, experts, top, dtype)
+
+
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("groups,top_groups,experts,top,tokens", [(8, 4, 256, 8, 601), (2, 1, 256, 8, 70), (32, 5, 256, 8, 70), (32, 2, 64, 4, 41), (12, 5, 96, 6, 70), (8, 3, 384, 8, 70),
+                                                                  (33, 4, 66, 3, 45), (44, 7, 132, 4, 45), (4, 2, 1024, 8, 45), (10, 3, 1000, 8, 45), (64, 9, 512, 8, 45)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_groups_of_all_kinds(sigmoid, groups, top_groups, experts, top, tokens, dtype):
+    check(logits(tokens, experts, 9, dtype), top, bias=torch.randn(experts, generator=torch.Generator().manual_seed(10)), sigmoid=sigmoid, groups=groups, top_groups=top_groups)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("experts", [64, 100, 256, 1024])
+@pytest.mark.parametrize("options", [dict(), dict(sigmoid=True), dict(groups=4, top_groups=2)])
+def test_the_ends_of_the_numbers(dtype, experts, options):
+    """Zeros of both signs are the same, the largest numbers and infinity are ordered as the type has them, and what is out is never chosen."""
+    ends = torch.tensor([0.0, -0.0, 1e-40, -1e-40, torch.finfo(dtype).max, -torch.finfo(dtype).max, math.inf, -math.inf, math.nan, 700.0, -700.0, -720.0, 1.0])
+    x = ends[torch.randint(0, len(ends), (40, experts), generator=torch.Generator().manual_seed(11))].to(dtype)
+    check(x, 32 if experts > 64 else 20, **options)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("experts", [64, 256, 512])
+def test_a_first_number_off_the_alignment(dtype, experts):
+    x, bias = logits(70, experts, 12, dtype), torch.randn(experts, generator=torch.Generator().manual_seed(13))
+    room, other = torch.full((70 * experts + 1,), math.nan, dtype=dtype, device=DEV), torch.full((experts + 1,), math.nan, device=DEV)
+    room[1:], other[1:] = x.view(-1).to(DEV), bias.to(DEV)
+    for b in (None, bias):
+        r = ecfm.ecfm_route(room[1:].view(70, experts), 6, bias=None if b is None else other[1:])
+        assert r.ids.tolist() == ref.route(x.double().numpy(), 6, bias=None if b is None else b.tolist())[0]
+        if b is not None:
+            r = ecfm.ecfm_route(x.to(DEV), 6, bias=other[1:])
+            assert r.ids.tolist() == ref.route(x.double().numpy(), 6, bias=b.tolist())[0]

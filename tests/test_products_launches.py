@@ -33,10 +33,11 @@ for odd in (1, -3, 255, (1 << 40) + 1):
 def route(tokens, per=64, experts=64, room=1 << 40):
     o = ecfm._RouteOpts(at, None, per, tokens, experts, 4, ecfa.F32, 0, 1, 1, 1, 1.0, 0)
     return launched(lib.ecfm_route(o, at, at, at, at, at, at, room, None))
-assert [route(t) for t in (0, 1, 64, 65, 16384, 16385, 1 << 22)] == [(0, n) for n in (1, 1, 1, 2, 2, 3, 3)]
+assert [route(t) for t in (0, 1, 32, 33, 65535, 65536, 1 << 22)] == [(0, n) for n in (1, 1, 1, 2, 2, 3, 3)]
+assert [route(t, 512, 512) for t in (16, 17, 65535, 65536)] == [(0, n) for n in (1, 2, 2, 3)]
 need = lib.ecfm_route_workspace_bytes
-for t in (65, 16384, 16385, 1 << 22):
-    assert route(t, room=need(t, 64, 4)) == (0, 2 if t <= 16384 else 3) and route(t, room=need(t, 64, 4) - 1) == (ecf8.E_CAPACITY, 0)
+for t in (33, 511, 513, 16384, 16385, 65535, 65536, 1 << 22):
+    assert route(t, room=need(t, 64, 4)) == (0, 2 if t <= 65535 else 3) and route(t, room=need(t, 64, 4) - 1) == (ecf8.E_CAPACITY, 0)
 def gate(rows, cols, stride, group): return launched(lib.ecfm_gate(at, at, ecfa.BF16, rows, cols, stride, stride, group, at, at, None))
 for group in (0, 128):
     assert gate(5, 256, 256, group) == (0, 1) and gate(1, 256, 7, group) == (0, 1) and gate(2, 256, 7, group) == (E, 0)
