@@ -27,8 +27,8 @@ struct ProductArgs {
     uint32_t f32, wide, lines;                     // Y in fp32; four elements of Y may be stored at once; BF16, and eight (n a multiple of eight)
 };
 
-struct Rows {                                      // m0 .. m1 of Y, expert e
-    uint32_t e, m0, m1;
+struct Rows {                                      // m0 .. m1 of Y, expert e, whose rows end at `end`
+    uint32_t e, m0, m1, end;
 };
 
 __device__ inline uint32_t cut(int32_t v, uint32_t m) { return v < 0 ? 0 : (uint32_t)v > m ? m : (uint32_t)v; }
@@ -70,14 +70,17 @@ struct Tiles {
         all = all < a.m_tiles ? all : a.m_tiles;               // (starts that fall could claim more)
     }
 
-    // false: there is no tile t
-    __device__ bool find(const ProductArgs &a, uint32_t t, Rows *r) const
+    // false: there is no tile t; else its expert's first tile and how many these are
+    __device__ bool find(const ProductArgs &a, uint32_t t, Rows *r, uint32_t *t0 = nullptr, uint32_t *tn = nullptr) const
     {
         if (t >= all) return false;
         if (!a.starts) {
             r->e = 0;
             r->m0 = t * BM;
             r->m1 = a.m - r->m0 < BM ? a.m : r->m0 + BM;
+            r->end = a.m;
+            if (t0) *t0 = 0;
+            if (tn) *tn = all;
             return true;
         }
         const uint64_t hit = __ballot(upto > t);
@@ -91,6 +94,9 @@ struct Tiles {
                 r->e = e;
                 r->m0 = b + (t - before) * BM;
                 r->m1 = b + n - r->m0 < BM ? b + n : r->m0 + BM;
+                r->end = b + n;
+                if (t0) *t0 = before;
+                if (tn) *tn = tiles;
                 return true;
             }
             before += tiles;

@@ -108,16 +108,23 @@ __global__ __launch_bounds__(512, 2) void ecfm_many_kernel(const ProductArgs a)
     const uint32_t wn = wave % WAVES_N, wm = wave / WAVES_N;
 
     // Workgroups go to the eight dies in turn.  A die gets a run of tiles that lie together, eight along n by some along m, so that its cache serves
-    // rows of W and X to several of them; its workgroups take them in turn.
+    // rows of W and X to several of them; its workgroups take them in turn.  Of the same expert up to HIGH along m are neighbours: those that read the same W
+    // are taken at the same time, and mostly by the same workgroups again (4096 tokens of 256 experts 1790 -> 1750 us, against eight along n first).
+    constexpr uint32_t HIGH = 4;
     const Tiles<BM> tiles(a);
     const uint32_t all = tiles.all * a.n_tiles, die = blockIdx.x % 8, share = all / 8 + (die < all % 8), each = gridDim.x / 8;
     const uint32_t run = die * (all / 8) + (die < all % 8 ? die : all % 8);
     const auto locate = [&](uint32_t i, Rows *r, uint32_t *n0) {
         if (i >= share) return false;
         const uint32_t group = (run + i) / (8 * tiles.all), first = group * 8, wide = a.n_tiles - first < 8 ? a.n_tiles - first : 8;
-        const uint32_t in = run + i - group * 8 * tiles.all;
-        *n0 = (first + in % wide) * BN;
-        return tiles.find(a, in / wide, r);
+        const uint32_t in = run + i - group * 8 * tiles.all, t = in / wide;
+        uint32_t t0, tn;
+        if (!tiles.find(a, t, r, &t0, &tn)) return false;
+        const uint32_t base = t - (t - t0) % HIGH, high = t0 + tn - base < HIGH ? t0 + tn - base : HIGH, w = in - base * wide, n = w / high, end = r->end;
+        *n0 = (first + n) * BN;
+        r->m0 = r->m0 + (base + (w - n * high)) * BM - t * BM;
+        r->m1 = end - r->m0 < BM ? end : r->m0 + BM;
+        return true;
     };
     // Rows of X that this lane loads: lane / 8 + 8 * ... (outside of X: the first); whether those that it multiplies, lane % 16 + 16 * j, are rows of X
     const auto rows_of_tile = [&](const Rows &r, uint32_t *x_row) {
