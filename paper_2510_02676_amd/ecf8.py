@@ -19,6 +19,8 @@ if not os.path.exists(LIB_PATH):
                       "(or __graft_entry__.build()) first; there is no fallback path")
 _lib = ctypes.CDLL(LIB_PATH)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+# torch.cuda.current_device() without the look whether CUDA is there yet, for those who hold one of its tensors
+_device_now = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 OK, E_ARG, E_FORMAT, E_CAPACITY, E_ALIGN, E_HIP, E_NOMEM = 0, -1, -2, -3, -4, -5, -6
 

@@ -65,7 +65,7 @@ def _stream_ptr(fn, on, stream):
     if stream is not None:
         if stream.device_index != on:
             raise _bad(fn)
-    elif on < 0 or torch.cuda.current_device() != on:
+    elif on < 0 or _e._device_now() != on:
         raise _bad(fn)
     elif _e._raw_stream is not None:
         return _e._raw_stream(on)

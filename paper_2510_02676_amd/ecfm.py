@@ -14,6 +14,7 @@ from . import ecf8 as _e
 from .ecfa import _BYTES, _DTYPE, _bad, _empty, _stream_ptr
 
 _lib = _e._lib
+_U32 = (1 << 32) - 1
 _vp, _u64, _u32, _i64, _f32 = ctypes.c_void_p, ctypes.c_uint64, ctypes.c_uint32, ctypes.c_int64, ctypes.c_float
 
 
@@ -55,8 +56,8 @@ def _dense(fn, t, dtype, shape, on):
 
 def _matrix(fn, y, rows, cols, on):
     """A (rows, cols) tensor of fp32 or BF16 as the C structure: any distance between rows, columns next to each other."""
-    shape, stride, dtype = y.shape, y.stride(), _DTYPE.get(y.dtype)
-    if len(shape) != 2 or shape[0] != rows or shape[1] != cols or dtype is None or (cols > 1 and stride[1] != 1) or y.get_device() != on or rows >= 1 << 32:
+    stride, dtype = y.stride(), _DTYPE.get(y.dtype)
+    if y.shape != (rows, cols) or dtype is None or (stride[1] != 1 and cols > 1) or y.get_device() != on or rows > _U32:
         raise _bad(fn)
     return _Y(y.data_ptr(), stride[0], rows, dtype)
 
@@ -173,7 +174,8 @@ def ecfm_gate(g, u, group=0, q=None, scale=None, stream=None):
         raise _bad("ecfm_gate")
     at = _stream_ptr("ecfm_gate", on, stream)
     rows, cols = shape
-    if cols > 1 and (g.stride(1) != 1 or u.stride(1) != 1):
+    g_stride, u_stride = g.stride(), u.stride()
+    if cols > 1 and (g_stride[1] != 1 or u_stride[1] != 1):
         raise _bad("ecfm_gate")
     want = (rows, cols // 128) if group else (rows,)
     if q is None:
@@ -182,7 +184,7 @@ def ecfm_gate(g, u, group=0, q=None, scale=None, stream=None):
         scale = _empty(want, torch.float32, g.device, stream)
     if q.dtype not in _BYTES or q.shape != shape or not q.is_contiguous() or q.get_device() != on:
         raise _bad("ecfm_gate")
-    rc = _gate(g.data_ptr(), u.data_ptr(), dtype, rows, cols, g.stride(0), u.stride(0), group, q.data_ptr(), _dense("ecfm_gate", scale, torch.float32, want, on), at)
+    rc = _gate(g.data_ptr(), u.data_ptr(), dtype, rows, cols, g_stride[0], u_stride[0], group, q.data_ptr(), _dense("ecfm_gate", scale, torch.float32, want, on), at)
     if rc:
         _e._check("ecfm_gate", rc)
     return q, scale
@@ -192,18 +194,19 @@ def ecfm_combine(y, place, weights, add=None, out=None, dtype=torch.bfloat16, st
     """out[t] = add[t] + sum over j of weights[t][j] * y[place[t][j]]: y (rows, cols), add and out (tokens, cols) BF16 or fp32 (out allocated in
     `dtype` if absent, and may be add), place (tokens, top) int32, weights (tokens, top) fp32."""
     on = y.get_device()
-    if y.dim() != 2 or place.dim() != 2:
+    shape, pairs = y.shape, place.shape
+    if len(shape) != 2 or len(pairs) != 2:
         raise _bad("ecfm_combine")
     at = _stream_ptr("ecfm_combine", on, stream)
-    (tokens, top), cols = place.shape, y.shape[1]
+    (rows, cols), (tokens, top) = shape, pairs
     if out is None:
         if dtype not in _DTYPE:
             raise _bad("ecfm_combine")
         out = _empty((tokens, cols), dtype, y.device, stream)
-    if tokens >= 1 << 32 or top >= 1 << 32 or cols >= 1 << 32:
+    if tokens > _U32 or top > _U32 or cols > _U32:
         raise _bad("ecfm_combine")
-    rc = _combine(_matrix("ecfm_combine", y, y.shape[0], cols, on), _dense("ecfm_combine", place, torch.int32, (tokens, top), on),
-                  _dense("ecfm_combine", weights, torch.float32, (tokens, top), on), tokens, top, cols,
+    rc = _combine(_matrix("ecfm_combine", y, rows, cols, on), _dense("ecfm_combine", place, torch.int32, pairs, on),
+                  _dense("ecfm_combine", weights, torch.float32, pairs, on), tokens, top, cols,
                   None if add is None else _matrix("ecfm_combine", add, tokens, cols, on), _matrix("ecfm_combine", out, tokens, cols, on), at)
     if rc:
         _e._check("ecfm_combine", rc)
