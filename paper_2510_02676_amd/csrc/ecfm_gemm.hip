@@ -95,7 +95,7 @@ __device__ const u32x4 zeros[1] = {};
 // are read from unlike banks.  Scales come by eight blocks of a row: block by block they would be as many requests to memory as the operands are
 // (8192 x 14336 x 4096: 531 us, 466 so).
 // 256 x 256: 2.36 PFLOP/s at 8192 x 14336 x 4096, matrix cores 59 % of the time busy at 1.85 GHz, where the power holds the card (fewer cycles did
-// not take less time).  128 x 256, 4096 tokens: 6.4 TB/s of W, which is read once for each 128 rows of an expert.  64 x 256, 48 tokens: 6.07 TB/s.
+// not take less time).  128 x 256, 4096 tokens: 6.7 TB/s beyond the dies' caches, W once for each 128 rows of an expert.  64 x 256, 48 tokens: 6.07 TB/s.
 template <uint32_t BM, uint32_t BN, uint32_t WAVES_N, uint32_t STAGES>
 __global__ __launch_bounds__(512, 2) void ecfm_many_kernel(const ProductArgs a)
 {
@@ -109,8 +109,9 @@ __global__ __launch_bounds__(512, 2) void ecfm_many_kernel(const ProductArgs a)
 
     // Workgroups go to the eight dies in turn.  A die gets a run of tiles that lie together, eight along n by some along m, so that its cache serves
     // rows of W and X to several of them; its workgroups take them in turn.  Of the same expert up to HIGH along m are neighbours: those that read the same W
-    // are taken at the same time, and mostly by the same workgroups again (4096 tokens of 256 experts 1790 -> 1750 us, against eight along n first).
-    constexpr uint32_t HIGH = 4;
+    // are taken at the same time, and mostly by the same workgroups again (4096 tokens of 256 experts 1790 -> 1750 us, against eight along n first; with
+    // tiles of 128 along n 2021 -> 2237, so these go along n first).
+    constexpr uint32_t HIGH = BN == 256 ? 4 : 1;
     const Tiles<BM> tiles(a);
     const uint32_t all = tiles.all * a.n_tiles, die = blockIdx.x % 8, share = all / 8 + (die < all % 8), each = gridDim.x / 8;
     const uint32_t run = die * (all / 8) + (die < all % 8 ? die : all % 8);
@@ -423,7 +424,7 @@ int check(const ecfm_weights *w, const ecfm_x *x, const ecfm_y *y, ProductArgs *
 //   8192 x 14336 x 4096                256 x 256 411, 128 x 256 479, 128 x 128 601
 //   1 token of 8 experts, 4096 x 7168  64 x 128 44.2, 16 x 64 42.8, 64 x 256 53.5
 //   48 tokens, 256 of 7168 x 2048      64 x 256 417, 16 x 64 439, 128 x 128 419
-//   4096 tokens, 256 of 4096 x 7168    128 x 256 1788, 128 x 128 1975, 256 x 256 2179
+//   4096 tokens, 256 of 4096 x 7168    128 x 256 1750, 128 x 128 1975, 256 x 256 2179
 struct Shape {
     uint32_t bm, bn;
     float tile, block;
