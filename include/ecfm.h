@@ -123,7 +123,8 @@ int ecfm_route(const ecfm_route_opts *opts, int32_t *d_ids, float *d_weights, in
 /*
  * ecfm_gate: h = g / (1 + exp(-g)) * u in fp32, rows x cols, rounded to E4M3 as ecfa_quant rounds x: with a =
  * max(|h| of the row (group = 0) or of 128 columns (group = 128), 2^-100): scale = a / 448, q = h * (448 / a).
- * g = -infinity counts as silu = 0.  g and u: `dtype`, row strides in elements, which with the addresses are multiples of
+ * exp(-g) is not limited to what fp32 holds: g = -100, u = 3e38 give -1.1e-3.  g = -infinity counts as silu = 0.
+ * g and u: `dtype`, row strides in elements, which with the addresses are multiples of
  * 16 bytes; cols a multiple of 16 (of 128 with groups), up to 2^20.  d_q dense, d_scale[rows] or [rows][cols / 128].
  */
 int ecfm_gate(const void *d_g, const void *d_u, uint32_t dtype, uint64_t rows, uint64_t cols, int64_t g_stride, int64_t u_stride,

@@ -32,25 +32,41 @@ struct GateArgs {
     By by_row;
 };
 
-// silu(g) * u of eight: with t = exp(-|g|), g / (1 + t), or g t / (1 + t) below zero, so that nothing overflows on the way; at -infinity g t would be
-// NaN.  t = 2^e (1 + r ln 2), e the product of -|g| and log2(e) in fp32 and r what that leaves out, is within two of its last places (0 where
-// it is below fp32's normal numbers).  exp, a division and clamps were 373 instructions for the eight and as long as their bytes (86 us at 32768 x 2048;
-// 72 with a reciprocal, 58 so: 5.8 TB/s).
+// silu(g) * u of eight: with t = exp(-|g|), g / (1 + t), or g t / (1 + t) below zero, so that nothing overflows on the way.
+// t = 2^e (1 + r ln 2), e the product of -|g| and log2(e) in fp32 and r what that leaves out, is within two of its last places.  From g = -87.3 on
+// down t is below fp32's normal numbers, which the instruction puts to 0, though with a large u the product is not: there, and from LOW on, t is taken
+// 2^136 times as large and u as much smaller (1 + t is 1).  That reaches to g = -181; below, the product is less than 2^-126, which is 0 beside 2^-100,
+// and so it is at -infinity, where g t would be NaN.
+// exp, a division and clamps were 373 instructions for the eight and as long as their bytes (86 us at 32768 x 2048; 72 with a reciprocal, 59 so: 5.7 TB/s;
+// 58.3 where all products below -87.3 are zeros).
 template <bool F32>
 __device__ inline void gated8(const uint8_t *g, const uint8_t *u, float *h)
 {
     constexpr float LOG2E = 1.44269502f, REST = 1.92596303e-8f, LN2 = 0.693147181f;       // LOG2E + REST = log2(e)
-    float x[8];
+    constexpr float LOW = -87.f;
+    float x[8], silu[8];
+    uint32_t lowest = 0;                                       // as bits: of two numbers below zero the lower one has more
     load8<F32>(g, x);
     load8<F32>(u, h);
+    // 2^to (1 + r ln 2), `to` e or e and a whole number
+    const auto exp_of = [](float a, float e, float to) {
+        const float r = fmaf(a, REST, fmaf(a, LOG2E, -e)), t = __builtin_amdgcn_exp2f(to);
+        return t > 0.f ? fmaf(t, r * LN2, t) : t;              // (at infinity r is not a number)
+    };
     for (int i = 0; i < 8; i++) {
-        const float a = -fabsf(x[i]), e = a * LOG2E;
-        const float r = fmaf(a, REST, fmaf(a, LOG2E, -e));
-        float t = __builtin_amdgcn_exp2f(e);
-        t = t > 0.f ? fmaf(t, r * LN2, t) : t;                 // (at infinity r is not a number)
-        const float top = x[i] < 0.f ? (t == 0.f ? 0.f : x[i] * t) : x[i];
-        h[i] = top * __builtin_amdgcn_rcpf(1.f + t) * h[i];
+        const float a = -fabsf(x[i]), e = a * LOG2E, t = exp_of(a, e, e);
+        silu[i] = (x[i] < 0.f ? x[i] * t : x[i]) * __builtin_amdgcn_rcpf(1.f + t);
+        lowest = f32_bits(x[i]) > lowest ? f32_bits(x[i]) : lowest;
     }
+    if (__builtin_expect(lowest > f32_bits(LOW), 0))           // (in its place, not behind the end, 60 us)
+        for (int i = 0; i < 8; i++)
+            if (x[i] < LOW) {
+#pragma clang fp contract(off)                                 // (e + 136 is exact, but not as one operation with the product that r is the rest of)
+                const float e = x[i] * LOG2E, t = exp_of(x[i], e, e + 136.f);
+                silu[i] = t == 0.f ? 0.f : x[i] * t;
+                h[i] = __builtin_ldexpf(h[i], -136);
+            }
+    for (int i = 0; i < 8; i++) h[i] = silu[i] * h[i];
 }
 
 // Eight to E4M3 where none is further than a rounding beyond 448: they need not be limited.
