@@ -1,7 +1,7 @@
 """The experts of one layer with their weights compressed: any number of tokens, from hidden states and a router's logits to hidden states.
 
-Seven launches, or eight or nine where many tokens are sorted: all experts' weights are decoded into a buffer (``ecf8_decode_batched``), rows to E4M3
-(``ecfa_quant``), the tokens to their experts (``ecfm_route``), gate and up of every expert with its tokens (``ecfm_gemm_experts``), silu(gate) * up
+Seven launches, or eight or nine where many tokens are sorted: rows to E4M3 (``ecfa_quant``), all experts' weights are decoded into a buffer
+(``ecf8_decode_batched``), the tokens to their experts (``ecfm_route``), gate and up of every expert with its tokens (``ecfm_gemm_experts``), silu(gate) * up
 to E4M3 (``ecfm_gate``), down (``ecfm_gemm_experts``), and what came back to the tokens (``ecfm_combine``).  Nothing is allocated after
 construction and nothing looks at a tensor's values on the host, so a step can be captured in a graph.
 """
@@ -52,8 +52,8 @@ class CompressedExperts:
         """x (tokens, hidden), BF16 or fp32, logits (tokens, experts), add (tokens, hidden) or None, as of a shared expert -> (tokens, hidden) BF16, in a
         buffer that the next call writes again."""
         inner = self.h8.shape[1]
+        ecfa.ecfa_quant(x, 128, self.x8, self.x_scale, stream)     # (in front of the decode: this call refuses other devices and streams)
         ecf8.ecf8_decode_batched(self.decode, stream)
-        ecfa.ecfa_quant(x, 128, self.x8, self.x_scale, stream)
         r = ecfm.ecfm_route(logits, self.top, routes=self.routes, stream=stream, **self.options)
         ecfm.ecfm_gemm_experts(self.gate_up, r.starts, self.x8, self.x_scale, rows=r.rows, y=self.mid, stream=stream)
         ecfm.ecfm_gate(self.mid[:, :inner], self.mid[:, inner:], 128, self.h8, self.h_scale, stream)
