@@ -25,7 +25,9 @@ class CompressedExperts:
             for name, (rows, cols) in want.items():
                 hdr, blob, scale = e[name]
                 bad = (bad or (hdr.rows, hdr.cols) != (rows, cols) or blob.device != dev or scale.device != dev
-                       or scale.dtype != torch.float32 or scale.shape != (rows // 128, cols // 128))
+                       or scale.dtype != torch.float32 or scale.shape != (rows // 128, cols // 128)
+                       # (the decode reads as far as the header says)
+                       or blob.dtype != torch.uint8 or not blob.is_contiguous() or blob.numel() < hdr.total_size)
         if bad:
             raise ecf8.Ecf8Error("CompressedExperts", ecf8.E_ARG)
         n, pairs = len(experts), tokens * top
