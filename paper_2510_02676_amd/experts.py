@@ -17,6 +17,8 @@ class CompressedExperts:
     that run one after the other on a stream share (``layer.room``).  What a step would refuse is refused here."""
 
     def __init__(self, experts, tokens, top, room=None, **options):
+        if not experts:
+            raise ecf8.Ecf8Error("CompressedExperts", ecf8.E_ARG)
         inner, hidden = experts[0]["gate"][0].rows, experts[0]["gate"][0].cols
         dev = experts[0]["gate"][1].device
         want = {"gate": (inner, hidden), "up": (inner, hidden), "down": (hidden, inner)}

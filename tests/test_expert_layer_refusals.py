@@ -16,3 +16,9 @@ def test_a_refused_step_decodes_nothing(monkeypatch):
         with pytest.raises(ecf8.Ecf8Error) as e:
             layer(x, torch.zeros((5, 3)))
         assert e.value.code == ecf8.E_ARG and not queued
+
+
+def test_no_experts():
+    with pytest.raises(ecf8.Ecf8Error) as e:
+        CompressedExperts([], 5, 2)
+    assert e.value.code == ecf8.E_ARG
