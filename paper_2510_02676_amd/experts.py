@@ -22,7 +22,7 @@ class CompressedExperts:
         inner, hidden = experts[0]["gate"][0].rows, experts[0]["gate"][0].cols
         dev = experts[0]["gate"][1].device
         want = {"gate": (inner, hidden), "up": (inner, hidden), "down": (hidden, inner)}
-        bad = inner % 128 or hidden % 128 or dev.type == "cpu"
+        bad = inner % 128 or hidden % 128 or max(inner, hidden) > 1 << 20 or dev.type == "cpu"      # (2^20: what quant, gate and combine take)
         for e in experts:
             for name, (rows, cols) in want.items():
                 hdr, blob, scale = e[name]

@@ -24,3 +24,11 @@ def test_blobs_that_are_not_what_their_headers_say(name):
         assert refused([packed[0], dict(packed[1], **{name: (hdr, other, scale)})], 5, 2)
     longer = torch.cat((blob, blob[:7]))                                   # more than there is to read does no harm
     assert CompressedExperts([packed[0], dict(packed[1], **{name: (hdr, longer, scale)})], 5, 2).top == 2
+
+
+@pytest.mark.parametrize("inner,hidden", [(128, (1 << 20) + 128), ((1 << 20) + 128, 128)])
+def test_more_columns_than_a_steps_calls_take(inner, hidden):
+    """Rows to E4M3, the gate and the sum take up to 2^20.  The headers say no more than their sizes: what looks further at them refuses them for that."""
+    blob = torch.zeros(64, dtype=torch.uint8, device=DEV)
+    part = lambda rows, cols: (ecf8.Header(rows=rows, cols=cols), blob, torch.ones((rows // 128, cols // 128), device=DEV))  # noqa: E731
+    assert refused([{"gate": part(inner, hidden), "up": part(inner, hidden), "down": part(hidden, inner)}], 5, 1)
