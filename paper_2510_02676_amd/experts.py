@@ -50,7 +50,7 @@ class CompressedExperts:
         self.mid = empty((pairs, 2 * inner), torch.bfloat16)
         self.h8, self.h_scale = empty((pairs, inner), torch.uint8), empty((pairs, inner // 128), torch.float32)
         self.back, self.y = empty((pairs, hidden), torch.bfloat16), empty((tokens, hidden), torch.bfloat16)
-        ecfm.ecfm_route(empty((0, n), torch.float32), top, **options)                # refuses what a step's would, and chooses nothing
+        ecfm.ecfm_route(empty((0, n), torch.float32), top, routes=None, stream=None, **options)      # refuses what a step's would, and chooses nothing
 
     def __call__(self, x, logits, add=None, stream=None):
         """x (tokens, hidden), BF16 or fp32, logits (tokens, experts), add (tokens, hidden) or None, as of a shared expert -> (tokens, hidden) BF16, in a

@@ -32,3 +32,10 @@ def test_more_columns_than_a_steps_calls_take(inner, hidden):
     blob = torch.zeros(64, dtype=torch.uint8, device=DEV)
     part = lambda rows, cols: (ecf8.Header(rows=rows, cols=cols), blob, torch.ones((rows // 128, cols // 128), device=DEV))  # noqa: E731
     assert refused([{"gate": part(inner, hidden), "up": part(inner, hidden), "down": part(hidden, inner)}], 5, 1)
+
+
+@pytest.mark.parametrize("name", ["routes", "stream"])
+def test_options_that_a_step_gives_itself(name):
+    packed, _ = layer_weights(2, 128, 128, 6)
+    with pytest.raises(TypeError):
+        CompressedExperts(packed, 5, 2, **{name: None})
