@@ -3,7 +3,10 @@
  *
  * The fused products of ecf8.h take up to 64 rows.  For more (prompts, large batches), and for
  * experts whose numbers of rows only the device knows, a layer's weights are decoded into a
- * buffer (ecf8_decode, ecf8_decode_batched, ecf8_jit_*) and multiplied there:
+ * buffer (ecf8_decode, ecf8_decode_batched, ecf8_jit_*) and multiplied there.  Which call: compressed
+ * weights and up to 64 rows ecf8_gemm_fp8_scaled; weights that are bytes already ecfm_gemm, with few rows too (the
+ * ecf8_gemm_fp8_raw calls are the fused ones' yardstick on uncompressed weights: 17.2 us against 14.1 for one row
+ * of 14336 x 4096, 18.4 against 15.1 for 16, block scales, results in fp32, inputs past the caches).
  *
  *   ecfm_gemm          X W^T of E4M3 with block scales, any number of rows
  *   ecfm_gemm_experts  the same for every expert with the rows that were sent to it, one launch
@@ -54,7 +57,7 @@ typedef struct ecfm_x {
 } ecfm_x;
 
 /* The result: element n of row m is at d[m * row_stride + n], in elements; d and the rows are aligned
- * to their type. */
+ * to their type; rows do not overlap. */
 typedef struct ecfm_y {
     void *d;                       /* DEVICE                                            */
     int64_t row_stride;

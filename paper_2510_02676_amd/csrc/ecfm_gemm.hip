@@ -415,11 +415,16 @@ int check(const ecfm_weights *w, const ecfm_x *x, const ecfm_y *y, ProductArgs *
 }
 
 // What a round of workgroups, one to a compute unit, takes: the same for each tile and that for each block of 128 columns, in us, as measured with the card
-// full (cols 2048 to 14336).  The kernel is the one whose rounds come out shortest.  In us, that kernel and its neighbours, inputs past the caches:
+// full (cols 2048 to 14336).  The kernel is the one whose rounds come out shortest.  What these leave out: the bytes of W, which bound experts with few rows (the
+// estimates there are 31 us for 44, 517 for 417, 1531 for 1750; of one token the second best is chosen by 3 %); the stores of Y, which are
+// four elements at a time and less where n is not a multiple of eight or Y fp32 (4200 x 4400 x 272 23 us, fp32 33, 4200 x 4401 x 272 61 and 68); and
+// that a workgroup goes through all of K, however few tiles there are (the rows of 14336 columns below).
+// In us, that kernel and its neighbours, inputs past the caches:
 //   16 x 14336 x 4096                  16 x 64 15.1, 16 x 32 17.9, 64 x 128 19.1
 //   64 x 4096 x 4096                   32 x 32 12.2, 16 x 64 13.1, 64 x 128 18.6
 //   777 x 1001 x 2064                  32 x 64 12.0, 32 x 32 13.7, 64 x 128 14.2
 //   200 x 4096 x 4096                  64 x 128 18.3, 128 x 128 21.2, 32 x 64 28.5
+//   64 x 4096 x 14336                  34, 128 rows 47, 256 rows 55, 512 rows 58 (bytes: 8.7, 8.9, 9.9, 20 with the products)
 //   2048 x 4096 x 4096                 128 x 256 38, 128 x 128 46, 256 x 256 62
 //   8192 x 14336 x 4096                256 x 256 411, 128 x 256 479, 128 x 128 601
 //   1 token of 8 experts, 4096 x 7168  64 x 128 44.2, 16 x 64 42.8, 64 x 256 53.5
